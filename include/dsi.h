@@ -272,6 +272,110 @@ dsi_status dsi_accept_noalloc(void* stream, int32_t n_windows, int32_t k, int32_
                               const float* d_u, float temperature, int32_t mode,
                               int32_t* d_n_accepted, int32_t* d_next_token);
 
+/* A cache as dsi_kv_create's, its keys and values in the caller's device
+ * memory: d_k and d_v of nbytes bytes each (dsi_kv_bytes says how many),
+ * 16-byte aligned, which must live as long as the cache.  For servers that
+ * plan memory themselves, or read and write the cache with kernels of their
+ * own: K is [n_layers][n_windows][n_kv_heads][P/32][head_dim/32][32][32], in
+ * blocks of 32 positions with the position before the dim, V
+ * [n_layers][n_windows][n_kv_heads][P/32][head_dim][32], P = max_len rounded
+ * up to a multiple of 64, in kvdtype.  What the memory holds at first does not
+ * matter.  Such a caller does not change positions that a fork shares (below). */
+dsi_status dsi_kv_bytes(dsi_model* m, int32_t n_windows, int32_t max_len, size_t* bytes);
+dsi_status dsi_kv_wrap(dsi_model* m, int32_t n_windows, int32_t max_len, void* d_k, void* d_v, size_t nbytes,
+                       dsi_kv** out);
+
+/* Fork a window: windows window0 .. window0+n_windows-1 (src not among them)
+ * take the first len positions of window src, keys and values of every layer,
+ * and length len; len = -1: all that src holds when the copy runs.  A prompt
+ * then runs once, whatever the number of servers (Section 3.1, "KV cache")
+ * that follow it.  What the windows held before is given up; their rows behind
+ * len keep what they hold.  A len above src's length leaves them empty and is
+ * reported by the next synchronising call (DSI_EINVAL).  Stream-ordered;
+ * allocates nothing.
+ * The library remembers which positions a window still has in common with the
+ * window it was forked from: they end where either is rolled back, forked into
+ * or imported to.  dsi_verify, dsi_verify_tree and dsi_attend read the
+ * positions that consecutive windows of a call have in common with one
+ * window (in the call or not) once for all of them, from 128 positions on.
+ * Results then differ in rounding from those of a window by itself. */
+dsi_status dsi_kv_fork(dsi_kv* kv, int32_t src, int32_t window0, int32_t n_windows, int32_t len);
+
+/* Largest n_windows*rows of one dsi_attend. */
+#define DSI_MAX_ATTEND_ROWS 1024
+
+/* The attention step of one layer alone, for a server with projections of its
+ * own: caches `rows` keys and values for each of n_windows windows and attends
+ * from as many queries, out = softmax(q K^T / sqrt(head_dim)) V with query
+ * head h on KV head h / (n_heads / n_kv_heads).  Row i of window b sits at
+ * position L_b + i and sees [0, L_b + i].  Positions are the caller's business:
+ * q and k come rotated.  rows = 1 is a decoding step.
+ *   layer          the layer whose keys and values these are
+ *   d_q            [n_windows*rows][n_heads][head_dim] fp32, 16-byte aligned
+ *   d_k, d_v       [n_windows*rows][n_kv_heads][head_dim] fp32, rounded to
+ *                  kvdtype (nearest even) and stored at slots L_b ..
+ *   commit         if nonzero, the windows' lengths become L_b + rows (with the
+ *                  last layer of a step; a later call overwrites rows that were
+ *                  not committed)
+ *   d_out          [n_windows*rows][n_heads][head_dim] fp32, 16-byte aligned
+ * The model's weights are not used and need not be set.  Runs on the model's
+ * stream; its first call of a size allocates (capture later ones).  Fails with
+ * DSI_ECAPACITY if a length + rows may exceed max_len.
+ * Numerics: fp32-accurate queries and probabilities against the cache's type,
+ * fp32 sums.  A key or value of a row that is not finite reaches only the rows
+ * that see it. */
+typedef struct {
+  int32_t layer, window0, n_windows, rows;
+  const float* d_q;
+  const float* d_k;
+  const float* d_v;
+  int32_t commit;
+  float* d_out;
+} dsi_attend_args;
+
+dsi_status dsi_attend(dsi_model* m, dsi_kv* kv, const dsi_attend_args* args);
+
+/* Alternatives per row at most. */
+#define DSI_MAX_TOP 64
+
+/* Log probabilities from logits (dsi_verify's d_logits_out, or a server's
+ * own), with p = softmax(z / temperature) of each row:
+ *   d_logits       [rows][ld], ld >= vocab entries apart, of type dtype
+ *                  (DSI_F32 or DSI_BF16); no alignment beyond the type's
+ *   d_targets      [rows] int32 (nullable without d_logprob): a token per row
+ *   d_logprob      [rows] fp32 (nullable): log p(target); NaN for a target
+ *                  outside [0, vocab), such as -1 for a row without one
+ *   d_entropy      [rows] fp32 (nullable): -sum p log p in nats
+ *   n_top          alternatives per row, 0..DSI_MAX_TOP, at most vocab
+ *   d_top_ids      [rows][n_top] int32: the largest logits, descending, ties
+ *                  to the lowest id
+ *   d_top_logprobs [rows][n_top] fp32: their log p
+ *   d_ws, ws_bytes caller's workspace of at least dsi_logprobs_workspace bytes,
+ *                  8-byte aligned, for this call's work alone
+ * Masked entries (-inf) have probability 0 and log probability -inf, and come
+ * last among the alternatives, in id order.  A row with a NaN or +inf logit,
+ * or of -inf only, has NaN for every probability; its NaN entries are no
+ * alternatives (id -1 where nothing is left).  Sums over a row are in fp64 but
+ * for runs of 16 entries.  rows = 0 does nothing.  Stream-ordered, allocates
+ * nothing, and calls with workspaces of their own may overlap.  The current
+ * device is the stream's. */
+typedef struct {
+  int32_t rows, vocab, dtype, n_top;
+  int64_t ld;
+  const void* d_logits;
+  const int32_t* d_targets;
+  float temperature;
+  float* d_logprob;
+  float* d_entropy;
+  int32_t* d_top_ids;
+  float* d_top_logprobs;
+  void* d_ws;
+  size_t ws_bytes;
+} dsi_logprobs_args;
+
+dsi_status dsi_logprobs_workspace(int32_t rows, int32_t vocab, int32_t n_top, size_t* bytes);
+dsi_status dsi_logprobs(void* stream, const dsi_logprobs_args* args);
+
 /* Roll a window back to new_len (DSI terminates the threads that built on a
  * rejected token, Algorithm 1; their cache rows become dead).  Stream-ordered;
  * new_len must be >= 0 and not above the window's current length (checked on

@@ -179,14 +179,16 @@ __global__ __launch_bounds__(256) void k_rmsnorm_pack(float* __restrict__ x, con
   norm_row(v, d, m, gain, eps, wtype, pack, sh);
 }
 
-__global__ void k_kv_rollback(int* lens, int window, int new_len, int* err) {
-  if (threadIdx.x == 0 && blockIdx.x == 0) {
-    if (new_len < 0 || new_len > lens[window]) atomicOr(err, 4);
-    else lens[window] = new_len;
+__global__ void k_kv_rollback(ForkState f, int window, int new_len, int* err) {
+  if (threadIdx.x == 0) {
+    if (new_len < 0 || new_len > f.lens[window]) atomicOr(err, 4);
+    else f.lens[window] = new_len;
   }
+  fork_cut(f, window, new_len);
 }
-__global__ void k_kv_set(int* lens, int window, int v) {
-  if (threadIdx.x == 0 && blockIdx.x == 0) lens[window] = v;
+__global__ void k_kv_set(ForkState f, int window, int v) {
+  if (threadIdx.x == 0) f.lens[window] = v;
+  fork_cut(f, window, v);
 }
 // advance a window by n prompt tokens if every id is valid
 __global__ void k_kv_add_checked(int* lens, int window, const int* tokens, int n, int V, int* err) {
@@ -411,12 +413,12 @@ hipError_t launch_rmsnorm_pack(float* x, const float* delta, int S, size_t delta
   return hipGetLastError();
 }
 
-hipError_t launch_kv_rollback(int* lens, int window, int new_len, int* err, hipStream_t s) {
-  hipLaunchKernelGGL(k_kv_rollback, dim3(1), dim3(64), 0, s, lens, window, new_len, err);
+hipError_t launch_kv_rollback(const ForkState& f, int window, int new_len, int* err, hipStream_t s) {
+  hipLaunchKernelGGL(k_kv_rollback, dim3(1), dim3(64), 0, s, f, window, new_len, err);
   return hipGetLastError();
 }
-hipError_t launch_kv_set(int* lens, int window, int new_len, hipStream_t s) {
-  hipLaunchKernelGGL(k_kv_set, dim3(1), dim3(64), 0, s, lens, window, new_len);
+hipError_t launch_kv_set(const ForkState& f, int window, int new_len, hipStream_t s) {
+  hipLaunchKernelGGL(k_kv_set, dim3(1), dim3(64), 0, s, f, window, new_len);
   return hipGetLastError();
 }
 hipError_t launch_kv_add_checked(int* lens, int window, const int* tokens, int n, int V, int* err,

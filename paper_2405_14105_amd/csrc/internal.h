@@ -374,9 +374,103 @@ hipError_t launch_tree_compact(const TreeArgs& a, int kv_bf16, void* kc, void* v
                                size_t layer_elems, size_t win_elems, int n_kv, int hd, int maxlen,
                                hipStream_t s);
 
+// log probabilities of rows of logits (logprobs.hip)
+struct LpStat {         // of one run of a row
+  double rest, t;       // sums of e^x over the entries below the maximum, and of e^x log2(e) x
+  float m, cnt;         // the maximum, and how many entries equal it
+};
+struct LogprobArgs {
+  int rows, V, n;       // n: alternatives per row, at most kMaxTop
+  int bf16;             // type of z
+  size_t ld;            // entries between rows
+  const void* z;
+  const int* tokens;    // [rows], with logprob
+  float k2;             // log2(e) / T
+  double inv_temperature;
+  float* logprob;       // [rows], nullable
+  float* entropy;       // [rows], nullable
+  int* top_ids;         // [rows][n]
+  float* top_logprob;   // [rows][n]
+  // set by launch_logprobs
+  int U;                // runs per row
+  LpStat* stat;         // workspace [rows][U]
+  unsigned long long* keys;   // workspace [rows][U][n]
+};
+constexpr int kMaxTop = 64;
+constexpr int kMaxLogprobRows = 1 << 24, kMaxLogprobVocab = 1 << 30;
+size_t logprobs_workspace_bytes(int rows, int V, int n);
+hipError_t launch_logprobs(LogprobArgs a, void* ws, hipStream_t s);
+
+// Forked windows (share.hip).  root[w] is the window that w was last forked
+// from and shared[w] the number of leading positions that the two still hold
+// alike: at most both lengths, and less after a rollback of either.
+struct ForkState {
+  int* lens;
+  int* root;            // both [n_windows]; shared 0: nothing
+  int* shared;
+  int n_windows;
+};
+// a window's rows from new_len on may change from now on
+__device__ inline void fork_cut(const ForkState& f, int window, int new_len) {
+  for (int w = threadIdx.x; w < f.n_windows; w += blockDim.x)
+    if (w == window || f.root[w] == window) f.shared[w] = f.shared[w] < new_len ? f.shared[w] : new_len;
+}
+struct ForkArgs {
+  ForkState f;
+  void* kc;             // cache bases; layers layer_bytes and windows win_bytes apart
+  void* vc;
+  size_t layer_bytes, win_bytes;
+  int n_layers, n_kv, hd, maxlen, esz;
+  int src, window0, n;
+  int len;              // positions taken, -1: the source's length
+  int* err;
+};
+hipError_t launch_kv_fork(const ForkArgs& a, int max_len, hipStream_t s);
+hipError_t launch_fork_cut(const ForkState& f, int window, int new_len, hipStream_t s);
+
+// Attention of B windows' rows, the prefix that windows forked from one window
+// share read once for all of them (share.hip).
+constexpr int kMaxForkGroups = kMaxRows / 2;
+struct ShareGroup {
+  int first, count;     // windows of the call
+  int root;             // the window forked from
+};
+struct ShareArgs {
+  const float* q;       // [B * R][n_heads * hd]
+  const void* kc;       // layer base
+  const void* vc;
+  ForkState f;
+  int window0, B, R;
+  int n_heads, n_kv, maxlen;
+  float scale;
+  const unsigned long long* anc;   // nullable: token-tree rows (AttnArgs)
+  int n_groups;
+  ShareGroup group[kMaxForkGroups];
+  int p_tiles, p_chunks;   // of a group's prefix: query tiles (16 rows x heads) and key chunks at most
+  int t_tiles, t_chunks;   // of a window's own keys
+  float* part_o;        // [p_chunks + t_chunks][B * R * n_heads][hd]
+  float2* part_ml;      // [p_chunks + t_chunks][B * R * n_heads]
+  PackRef out;          // O-projection input pack, or
+  int wtype;
+  float* out_rows;      // [B * R][n_heads * hd] instead (nullable)
+};
+hipError_t launch_attention_shared(int kv_bf16, int hd, const ShareArgs& a, hipStream_t s);
+// rows' keys and values [B * R][n_kv * hd] into the cache behind each window's length
+struct AppendArgs {
+  const float* k;
+  const float* v;
+  void* kc;             // layer base
+  void* vc;
+  int kv_bf16;
+  const int* lens;
+  int window0, B, R, n_kv, hd, maxlen;
+};
+hipError_t launch_kv_append(const AppendArgs& a, hipStream_t s);
+hipError_t launch_kv_advance(int* lens, int window0, int B, int rows, hipStream_t s);
+
 // KV and misc (elementwise.hip)
-hipError_t launch_kv_rollback(int* lens, int window, int new_len, int* err, hipStream_t s);
-hipError_t launch_kv_set(int* lens, int window, int new_len, hipStream_t s);
+hipError_t launch_kv_rollback(const ForkState& f, int window, int new_len, int* err, hipStream_t s);
+hipError_t launch_kv_set(const ForkState& f, int window, int new_len, hipStream_t s);
 hipError_t launch_kv_add_checked(int* lens, int window, const int* tokens, int n, int V, int* err,
                                  hipStream_t s);
 // Prompt rows of one forward (n tokens): gpos (RowMap).  The window's length

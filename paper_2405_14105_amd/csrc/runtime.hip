@@ -184,9 +184,12 @@ struct dsi_kv {
   int n_windows = 0, max_len = 0, maxlen_pad = 0;
   void* k = nullptr;
   void* v = nullptr;
-  int* lens = nullptr;
+  bool owned = true;               // k and v are the library's
+  int* lens = nullptr;             // [3][n_windows]: lengths, then ForkState's root and shared
   std::vector<long long> hi, lo;   // host bounds on each window's length
+  std::vector<int> root;           // the window each was last forked from, or -1
   size_t win_elems = 0;            // elements of one (layer, window) of K (= of V)
+  ForkState forks() const { return ForkState{lens, lens + n_windows, lens + 2 * n_windows, n_windows}; }
 };
 
 namespace {
@@ -633,6 +636,74 @@ dsi_status plan_attention(dsi_model* m, dsi_kv* kv, int window0, int B, int R, A
   return ensure_attention(m, attention_plan(m, kv, kmax, B, R, p));
 }
 
+// Attention of windows that were forked from one window (share.hip): the runs
+// of consecutive windows of a call that share a prefix, and the partition.
+struct SharePlan {
+  ShareArgs a{};        // groups, tiles and chunks; the rest by share_args
+  size_t parts = 0;     // partial rows
+  bool any() const { return a.n_groups > 0; }
+};
+
+// The host knows which window each was forked from; how much of it is still
+// shared is known on the device when the attention runs, so the partition goes
+// by the cache's capacity.  About one workgroup per CU for the prefix, and two
+// for the windows' own keys, which are mostly short.
+SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, int R) {
+  SharePlan p;
+  ShareArgs& a = p.a;
+  a.window0 = window0;
+  a.B = B;
+  a.R = R;
+  auto run = [&](int i, int r) {   // windows from i on that are r or were forked from it
+    int j = i;
+    while (j < B && (window0 + j == r || kv->root[window0 + j] == r)) ++j;
+    return j - i;
+  };
+  int most = 0;
+  for (int i = 0; i < B && a.n_groups < kMaxForkGroups;) {
+    const int w = window0 + i;
+    int r = w, n = run(i, w);
+    if (kv->root[w] >= 0 && run(i, kv->root[w]) > n) n = run(i, r = kv->root[w]);
+    if (n > 1) {
+      a.group[a.n_groups++] = ShareGroup{i, n, r};
+      most = std::max(most, n);
+    }
+    i += n;
+  }
+  const int G = m->hq / m->hkv;
+  a.t_tiles = cdiv(G * R, 16);
+  a.t_chunks = std::min(std::max(1, 512 / (B * m->hkv * a.t_tiles)), cdiv(kv->max_len, 256));
+  if (a.n_groups) {
+    a.p_tiles = cdiv(G * R * most, 16);
+    a.p_chunks = std::min(std::max(1, 256 / (a.n_groups * m->hkv * a.p_tiles)), cdiv(kv->max_len, 256));
+  }
+  p.parts = (size_t)(a.p_chunks + a.t_chunks) * B * R * m->hq;
+  return p;
+}
+
+ShareArgs share_args(const dsi_model* m, const dsi_kv* kv, const SharePlan& p, int layer, const float* q) {
+  ShareArgs a = p.a;
+  a.q = q;
+  a.kc = kv_ptr(kv, kv->k, layer, 0);
+  a.vc = kv_ptr(kv, kv->v, layer, 0);
+  a.f = kv->forks();
+  a.n_heads = m->hq;
+  a.n_kv = m->hkv;
+  a.maxlen = kv->maxlen_pad;
+  a.scale = (float)(1.0 / sqrt((double)m->hd));
+  a.part_o = m->attn_o;
+  a.part_ml = m->attn_ml;
+  return a;
+}
+
+// what a captured step depends on of it
+void share_key(const SharePlan& p, std::vector<uint64_t>* key) {
+  const ShareArgs& a = p.a;
+  for (int x : {a.n_groups, a.p_tiles, a.p_chunks, a.t_tiles, a.t_chunks}) key->push_back((uint64_t)x);
+  for (int g = 0; g < a.n_groups; ++g)
+    for (int x : {a.group[g].first, a.group[g].count, a.group[g].root}) key->push_back((uint64_t)x);
+}
+
 // Whether a forward runs its layer GEMMs on the ring layouts: every bf16
 // forward of a model built with them (one to four row tiles, any number of
 // windows).  The ring kernels form each row's sums in the same order for
@@ -647,7 +718,8 @@ bool ring_forward(const dsi_model* m, const dsi_kv* kv, int mt) {
 // (nullable, device [M]): token-tree rows (RowMap::depth, AttnArgs::anc).
 dsi_status run_forward(dsi_model* m, dsi_kv* kv, const AttnPlan& ap, int window0, int B, int R,
                        const int* d_tokens, float* logits, int head_last_only, float* hidden,
-                       const int* depth = nullptr, const unsigned long long* anc = nullptr) {
+                       const int* depth = nullptr, const unsigned long long* anc = nullptr,
+                       const SharePlan* shared = nullptr) {
   hipStream_t s = m->stream;
   const int M = B * R;
   const int mt = cdiv(M, 16);
@@ -704,7 +776,14 @@ dsi_status run_forward(dsi_model* m, dsi_kv* kv, const AttnPlan& ap, int window0
     aa.wtype = m->wtype;
     aa.anc = anc;
     aa.waves = ap.waves;
-    {
+    if (shared && shared->any()) {
+      ShareArgs sa = share_args(m, kv, *shared, l, m->qbuf);
+      sa.anc = anc;
+      sa.out = m->pk_q;
+      sa.wtype = m->wtype;
+      Prof p(m, DSI_K_ATTN);
+      HIP_TRY(launch_attention_shared(m->kvb, m->hd, sa, s));
+    } else {
       Prof p(m, DSI_K_ATTN);
       HIP_TRY(launch_attention(m->kvb, m->hd, aa, s));
     }
@@ -1044,6 +1123,7 @@ dsi_status check_err_word(int* err, hipStream_t s) {
     if (h & 2) what += " verification input invalid (token id or q(d) <= 0);";
     if (h & 4) what += " rollback above the current length;";
     if (h & 8) what += " token-tree parent array invalid;";
+    if (h & 16) what += " fork beyond the source's length;";
     return fail(DSI_EINVAL, "device-detected input error:%s", what.c_str());
   }
   return DSI_OK;
@@ -1397,8 +1477,8 @@ dsi_status dsi_model_set_tensor(dsi_model* m, int32_t layer, int32_t id, const v
   return DSI_OK;
 }
 
-dsi_status dsi_kv_create(dsi_model* m, int32_t n_windows, int32_t max_len, dsi_kv** out) {
-  if (!m || !out) return fail(DSI_EINVAL, "null argument");
+// a cache object whose keys and values are still to come
+static dsi_status kv_new(dsi_model* m, int n_windows, int max_len, dsi_kv** out) {
   if (n_windows < 1 || max_len < 1) return fail(DSI_EINVAL, "n_windows and max_len must be >= 1");
   dsi_kv* kv = new (std::nothrow) dsi_kv();
   if (!kv) return fail(DSI_ENOMEM, "host allocation failed");
@@ -1409,12 +1489,24 @@ dsi_status dsi_kv_create(dsi_model* m, int32_t n_windows, int32_t max_len, dsi_k
   kv->win_elems = (size_t)m->hkv * kv->maxlen_pad * m->hd;
   kv->hi.assign(n_windows, 0);
   kv->lo.assign(n_windows, 0);
-  const size_t bytes = (size_t)m->L * n_windows * kv->win_elems * m->kvesz;
+  kv->root.assign(n_windows, -1);
+  *out = kv;
+  return DSI_OK;
+}
+static size_t kv_bytes(const dsi_kv* kv) {
+  return (size_t)kv->m->L * kv->n_windows * kv->win_elems * kv->m->kvesz;
+}
+
+dsi_status dsi_kv_create(dsi_model* m, int32_t n_windows, int32_t max_len, dsi_kv** out) {
+  if (!m || !out) return fail(DSI_EINVAL, "null argument");
+  dsi_kv* kv = nullptr;
+  DSI_TRY(kv_new(m, n_windows, max_len, &kv));
+  const size_t bytes = kv_bytes(kv);
   std::vector<void*> list;
   auto alloc = [&]() {
     dsi_status st = dev_alloc(list, &kv->k, bytes);
     if (st == DSI_OK) st = dev_alloc(list, &kv->v, bytes);
-    if (st == DSI_OK) st = dev_alloc(list, (void**)&kv->lens, (size_t)n_windows * sizeof(int));
+    if (st == DSI_OK) st = dev_alloc(list, (void**)&kv->lens, 3 * (size_t)n_windows * sizeof(int));
     if (st != DSI_OK) free_list(list);
     return st;
   };
@@ -1429,11 +1521,48 @@ dsi_status dsi_kv_create(dsi_model* m, int32_t n_windows, int32_t max_len, dsi_k
   return DSI_OK;
 }
 
+dsi_status dsi_kv_bytes(dsi_model* m, int32_t n_windows, int32_t max_len, size_t* bytes) {
+  if (!m || !bytes) return fail(DSI_EINVAL, "null argument");
+  dsi_kv* kv = nullptr;
+  DSI_TRY(kv_new(m, n_windows, max_len, &kv));
+  *bytes = kv_bytes(kv);
+  delete kv;
+  return DSI_OK;
+}
+
+dsi_status dsi_kv_wrap(dsi_model* m, int32_t n_windows, int32_t max_len, void* d_k, void* d_v, size_t nbytes,
+                       dsi_kv** out) {
+  if (!m || !out || !d_k || !d_v) return fail(DSI_EINVAL, "null argument");
+  if (((uintptr_t)d_k | (uintptr_t)d_v) & 15) return fail(DSI_EINVAL, "cache memory not 16-byte aligned");
+  dsi_kv* kv = nullptr;
+  DSI_TRY(kv_new(m, n_windows, max_len, &kv));
+  if (nbytes != kv_bytes(kv)) {
+    const size_t want = kv_bytes(kv);
+    delete kv;
+    return fail(DSI_EINVAL, "keys and values of this cache are %zu bytes each, got %zu", want, nbytes);
+  }
+  kv->owned = false;
+  kv->k = d_k;
+  kv->v = d_v;
+  std::vector<void*> list;
+  const dsi_status st = dev_alloc(list, (void**)&kv->lens, 3 * (size_t)n_windows * sizeof(int));
+  if (st != DSI_OK) {
+    free_list(list);
+    delete kv;
+    return st;
+  }
+  m->live_kv++;
+  *out = kv;
+  return DSI_OK;
+}
+
 dsi_status dsi_kv_destroy(dsi_kv* kv) {
   if (!kv) return DSI_OK;
   hipStreamSynchronize(kv->m->stream);
-  hipFree(kv->k);
-  hipFree(kv->v);
+  if (kv->owned) {
+    hipFree(kv->k);
+    hipFree(kv->v);
+  }
   hipFree(kv->lens);
   kv->m->live_kv--;
   kv->m->wide_wait = 0;
@@ -1490,6 +1619,8 @@ dsi_status dsi_verify(dsi_model* m, dsi_kv* kv, const dsi_verify_args* a, int32_
   float* logits = a->d_logits_out ? a->d_logits_out : m->logits;
   AttnPlan ap;
   DSI_TRY(plan_attention(m, kv, a->window0, B, k + 1, &ap));
+  const SharePlan sp = plan_shared(m, kv, a->window0, B, k + 1);
+  if (sp.any()) DSI_TRY(ensure_attention(m, sp.parts));
   m->last_window0 = a->window0;
   m->last_B = B;
   m->last_R = k + 1;
@@ -1511,7 +1642,7 @@ dsi_status dsi_verify(dsi_model* m, dsi_kv* kv, const dsi_verify_args* a, int32_
   va.err = m->err;
   verify_bind_workspace(va, m->vws, B * (k + 1), B, m->V);
   auto launches = [&]() -> dsi_status {
-    DSI_TRY(run_forward(m, kv, ap, a->window0, B, k + 1, a->d_tokens, logits, 0, a->d_hidden_out));
+    DSI_TRY(run_forward(m, kv, ap, a->window0, B, k + 1, a->d_tokens, logits, 0, a->d_hidden_out, nullptr, nullptr, &sp));
     Prof p(m, DSI_K_VERIFY);
     HIP_TRY(launch_verify(va, m->stream));
     return DSI_OK;
@@ -1521,7 +1652,7 @@ dsi_status dsi_verify(dsi_model* m, dsi_kv* kv, const dsi_verify_args* a, int32_
     // the model's lifetime except the attention partials, which are keyed)
     uint32_t tbits;
     memcpy(&tbits, &a->temperature, 4);
-    const std::vector<uint64_t> key = {
+    std::vector<uint64_t> key = {
         1u, (uint64_t)a->window0, (uint64_t)B, (uint64_t)k, (uint64_t)(uintptr_t)a->d_tokens,
         (uint64_t)(uintptr_t)a->d_q, (uint64_t)(uintptr_t)a->d_u, tbits, (uint64_t)a->mode,
         (uint64_t)a->commit, (uint64_t)(uintptr_t)logits, (uint64_t)(uintptr_t)a->d_hidden_out,
@@ -1530,6 +1661,7 @@ dsi_status dsi_verify(dsi_model* m, dsi_kv* kv, const dsi_verify_args* a, int32_
         (uint64_t)kv->n_windows, (uint64_t)kv->max_len, (uint64_t)kv->maxlen_pad,
         (uint64_t)ap.n_qtiles, (uint64_t)ap.chunk, (uint64_t)ap.n_chunks, (uint64_t)ap.waves,
         (uint64_t)(uintptr_t)m->attn_o, (uint64_t)(uintptr_t)m->attn_ml};
+    share_key(sp, &key);
     DSI_TRY(replay_or_capture(m, key, launches));
   } else {
     DSI_TRY(launches());
@@ -1561,6 +1693,8 @@ dsi_status dsi_verify_tree(dsi_model* m, dsi_kv* kv, const dsi_tree_args* a, int
   float* logits = a->d_logits_out ? a->d_logits_out : m->logits;
   AttnPlan ap;
   DSI_TRY(plan_attention(m, kv, a->window0, B, R, &ap));
+  const SharePlan sp = plan_shared(m, kv, a->window0, B, R);
+  if (sp.any()) DSI_TRY(ensure_attention(m, sp.parts));
   m->last_window0 = a->window0;
   m->last_B = B;
   m->last_R = R;
@@ -1595,7 +1729,7 @@ dsi_status dsi_verify_tree(dsi_model* m, dsi_kv* kv, const dsi_tree_args* a, int
   const size_t layer_elems = (size_t)kv->n_windows * kv->win_elems;
   auto launches = [&]() -> dsi_status {
     HIP_TRY(launch_tree_prep(ta, m->stream));
-    DSI_TRY(run_forward(m, kv, ap, a->window0, B, R, a->d_tokens, logits, 0, nullptr, m->tdepth, m->tanc));
+    DSI_TRY(run_forward(m, kv, ap, a->window0, B, R, a->d_tokens, logits, 0, nullptr, m->tdepth, m->tanc, &sp));
     Prof p(m, DSI_K_VERIFY);
     HIP_TRY(launch_verify_rowstats(va, m->stream));
     HIP_TRY(launch_tree_decide(ta, m->stream));
@@ -1605,7 +1739,7 @@ dsi_status dsi_verify_tree(dsi_model* m, dsi_kv* kv, const dsi_tree_args* a, int
     return DSI_OK;
   };
   if (m->use_graphs && m->prof_class == 0) {
-    const std::vector<uint64_t> key = {
+    std::vector<uint64_t> key = {
         2u, (uint64_t)a->window0, (uint64_t)B, (uint64_t)R, (uint64_t)(uintptr_t)a->d_tokens,
         (uint64_t)(uintptr_t)a->d_parent, (uint64_t)a->commit, (uint64_t)(uintptr_t)logits,
         (uint64_t)(uintptr_t)d_path, (uint64_t)(uintptr_t)d_n_accepted, (uint64_t)(uintptr_t)d_next_token,
@@ -1613,6 +1747,7 @@ dsi_status dsi_verify_tree(dsi_model* m, dsi_kv* kv, const dsi_tree_args* a, int
         (uint64_t)kv->n_windows, (uint64_t)kv->max_len, (uint64_t)kv->maxlen_pad,
         (uint64_t)ap.n_qtiles, (uint64_t)ap.chunk, (uint64_t)ap.n_chunks, (uint64_t)ap.waves,
         (uint64_t)(uintptr_t)m->attn_o, (uint64_t)(uintptr_t)m->attn_ml};
+    share_key(sp, &key);
     DSI_TRY(replay_or_capture(m, key, launches));
   } else {
     DSI_TRY(launches());
@@ -1746,12 +1881,142 @@ dsi_status dsi_accept_noalloc(void* stream, int32_t B, int32_t k, int32_t V, con
   return DSI_OK;
 }
 
+dsi_status dsi_kv_fork(dsi_kv* kv, int32_t src, int32_t window0, int32_t n_windows, int32_t len) {
+  if (!kv) return fail(DSI_EINVAL, "null kv");
+  if (src < 0 || src >= kv->n_windows) return fail(DSI_EINVAL, "bad window %d", src);
+  if (n_windows < 1 || window0 < 0 || window0 > kv->n_windows - n_windows)
+    return fail(DSI_EINVAL, "windows [%d, %lld) outside the cache's %d", window0, (long long)window0 + n_windows,
+                kv->n_windows);
+  if (src >= window0 && src < window0 + n_windows) return fail(DSI_EINVAL, "window %d forked into itself", src);
+  if (len < -1 || len > kv->hi[src])
+    return fail(DSI_EINVAL, "fork of %d positions above window %d's length (<= %lld)", len, src, kv->hi[src]);
+  const dsi_model* m = kv->m;
+  ForkArgs a{};
+  a.f = kv->forks();
+  a.kc = kv->k;
+  a.vc = kv->v;
+  a.win_bytes = kv->win_elems * m->kvesz;
+  a.layer_bytes = a.win_bytes * kv->n_windows;
+  a.n_layers = m->L;
+  a.n_kv = m->hkv;
+  a.hd = m->hd;
+  a.maxlen = kv->maxlen_pad;
+  a.esz = m->kvesz;
+  a.src = src;
+  a.window0 = window0;
+  a.n = n_windows;
+  a.len = len;
+  a.err = m->err;
+  (void)capturing(kv->m);
+  HIP_TRY(launch_kv_fork(a, len < 0 ? (int)kv->hi[src] : len, m->stream));
+  for (int w = window0; w < window0 + n_windows; ++w) {
+    kv->hi[w] = len < 0 ? kv->hi[src] : (long long)len;
+    kv->lo[w] = 0;
+    kv->root[w] = src;
+  }
+  return DSI_OK;
+}
+
+dsi_status dsi_attend(dsi_model* m, dsi_kv* kv, const dsi_attend_args* a) {
+  if (!m || !kv || !a || kv->m != m) return fail(DSI_EINVAL, "null argument or model / kv mismatch");
+  const int B = a->n_windows, R = a->rows;
+  if (a->layer < 0 || a->layer >= m->L) return fail(DSI_EINVAL, "bad layer %d", a->layer);
+  if (B < 1) return fail(DSI_EINVAL, "n_windows must be >= 1");
+  if (R < 1) return fail(DSI_EINVAL, "rows must be >= 1");
+  if ((long long)B * R > DSI_MAX_ATTEND_ROWS)
+    return fail(DSI_EINVAL, "n_windows*rows = %lld exceeds %d", (long long)B * R, DSI_MAX_ATTEND_ROWS);
+  if (a->window0 < 0 || a->window0 > kv->n_windows - B)
+    return fail(DSI_EINVAL, "windows [%d, %lld) outside the cache's %d", a->window0, (long long)a->window0 + B,
+                kv->n_windows);
+  if (!a->d_q || !a->d_k || !a->d_v || !a->d_out) return fail(DSI_EINVAL, "null queries, keys, values or output pointer");
+  if (((uintptr_t)a->d_q | (uintptr_t)a->d_out) & 15) return fail(DSI_EINVAL, "queries or output not 16-byte aligned");
+  (void)capturing(m);
+  for (int b = 0; b < B; ++b)
+    if (kv->hi[a->window0 + b] + R > kv->max_len)
+      return fail(DSI_ECAPACITY, "window %d: length (<= %lld) + %d exceeds max_len %d", a->window0 + b,
+                  kv->hi[a->window0 + b], R, kv->max_len);
+  const SharePlan sp = plan_shared(m, kv, a->window0, B, R);
+  DSI_TRY(ensure_attention(m, sp.parts));
+  ShareArgs sa = share_args(m, kv, sp, a->layer, a->d_q);
+  sa.out_rows = a->d_out;
+  AppendArgs pa{};
+  pa.k = a->d_k;
+  pa.v = a->d_v;
+  pa.kc = kv_ptr(kv, kv->k, a->layer, 0);
+  pa.vc = kv_ptr(kv, kv->v, a->layer, 0);
+  pa.kv_bf16 = m->kvb;
+  pa.lens = kv->lens;
+  pa.window0 = a->window0;
+  pa.B = B;
+  pa.R = R;
+  pa.n_kv = m->hkv;
+  pa.hd = m->hd;
+  pa.maxlen = kv->maxlen_pad;
+  Prof p(m, DSI_K_ATTN);
+  HIP_TRY(launch_kv_append(pa, m->stream));
+  HIP_TRY(launch_attention_shared(m->kvb, m->hd, sa, m->stream));
+  if (a->commit) {
+    HIP_TRY(launch_kv_advance(kv->lens, a->window0, B, R, m->stream));
+    for (int b = 0; b < B; ++b) kv->hi[a->window0 + b] += R;
+  }
+  return DSI_OK;
+}
+
+static dsi_status logprobs_sizes_ok(int32_t rows, int32_t vocab, int32_t n_top) {
+  if (rows < 0 || rows > kMaxLogprobRows) return fail(DSI_EINVAL, "rows must be in [0, %d]", kMaxLogprobRows);
+  if (vocab < 1 || vocab > kMaxLogprobVocab) return fail(DSI_EINVAL, "vocab must be in [1, %d]", kMaxLogprobVocab);
+  if (n_top < 0 || n_top > std::min(DSI_MAX_TOP, vocab))
+    return fail(DSI_EINVAL, "n_top must be in [0, %d] and at most vocab", DSI_MAX_TOP);
+  return DSI_OK;
+}
+
+dsi_status dsi_logprobs_workspace(int32_t rows, int32_t vocab, int32_t n_top, size_t* bytes) {
+  if (!bytes) return fail(DSI_EINVAL, "null argument");
+  DSI_TRY(logprobs_sizes_ok(rows, vocab, n_top));
+  *bytes = rows ? logprobs_workspace_bytes(rows, vocab, n_top) : 0;
+  return DSI_OK;
+}
+
+dsi_status dsi_logprobs(void* stream, const dsi_logprobs_args* a) {
+  if (!a) return fail(DSI_EINVAL, "null argument");
+  DSI_TRY(logprobs_sizes_ok(a->rows, a->vocab, a->n_top));
+  if (a->dtype != DSI_F32 && a->dtype != DSI_BF16) return fail(DSI_EINVAL, "bad dtype %d", a->dtype);
+  if (a->ld < a->vocab) return fail(DSI_EINVAL, "ld %lld below vocab %d", (long long)a->ld, a->vocab);
+  if (!(a->temperature > 0.f) || !isfinite(1.44269504088896340736f / a->temperature) || !isfinite(a->temperature))
+    return fail(DSI_EINVAL, "temperature must be positive");
+  if (!a->d_logprob && !a->d_entropy && !a->n_top) return fail(DSI_EINVAL, "no output asked for");
+  if (a->d_logprob && !a->d_targets) return fail(DSI_EINVAL, "log probabilities need d_targets");
+  if (a->n_top && (!a->d_top_ids || !a->d_top_logprobs)) return fail(DSI_EINVAL, "null output of the alternatives");
+  if (!a->rows) return DSI_OK;
+  if (!a->d_logits) return fail(DSI_EINVAL, "null logits");
+  if ((uintptr_t)a->d_logits % (a->dtype == DSI_BF16 ? 2 : 4)) return fail(DSI_EINVAL, "misaligned logits");
+  const size_t need = logprobs_workspace_bytes(a->rows, a->vocab, a->n_top);
+  if (!a->d_ws || ((uintptr_t)a->d_ws & 7) || a->ws_bytes < need)
+    return fail(DSI_EINVAL, "the workspace must hold %zu bytes, 8-byte aligned (got %zu)", need, a->ws_bytes);
+  LogprobArgs l{};
+  l.rows = a->rows;
+  l.V = a->vocab;
+  l.n = a->n_top;
+  l.bf16 = a->dtype == DSI_BF16;
+  l.ld = (size_t)a->ld;
+  l.z = a->d_logits;
+  l.tokens = a->d_targets;
+  l.k2 = 1.44269504088896340736f / a->temperature;
+  l.inv_temperature = 1.0 / (double)a->temperature;
+  l.logprob = a->d_logprob;
+  l.entropy = a->d_entropy;
+  l.top_ids = a->d_top_ids;
+  l.top_logprob = a->d_top_logprobs;
+  HIP_TRY(launch_logprobs(l, a->d_ws, (hipStream_t)stream));
+  return DSI_OK;
+}
+
 dsi_status dsi_kv_rollback(dsi_kv* kv, int32_t window, int32_t new_len) {
   if (!kv) return fail(DSI_EINVAL, "null kv");
   if (window < 0 || window >= kv->n_windows) return fail(DSI_EINVAL, "bad window %d", window);
   if (new_len < 0 || new_len > kv->hi[window])
     return fail(DSI_EINVAL, "rollback to %d above the window's length (<= %lld)", new_len, kv->hi[window]);
-  HIP_TRY(launch_kv_rollback(kv->lens, window, new_len, kv->m->err, kv->m->stream));
+  HIP_TRY(launch_kv_rollback(kv->forks(), window, new_len, kv->m->err, kv->m->stream));
   kv->hi[window] = new_len;
   kv->lo[window] = std::min(kv->lo[window], (long long)new_len);
   return DSI_OK;
@@ -1896,6 +2161,7 @@ static dsi_status kv_copy(dsi_kv* kv, int32_t window, int32_t layer, int32_t len
   dsi_model* m = kv->m;
   if (window < 0 || window >= kv->n_windows || layer < 0 || layer >= m->L || len < 0 || len > kv->max_len)
     return fail(DSI_EINVAL, "bad window / layer / len");
+  if (to_cache) HIP_TRY(launch_fork_cut(kv->forks(), window, 0, m->stream));
   HIP_TRY(launch_kv_copy(to_cache, m->kvb, kv_ptr(kv, kv->k, layer, window), kv_ptr(kv, kv->v, layer, window),
                          m->hkv, m->hd, kv->maxlen_pad, len, dk, dv, m->stream));
   return DSI_OK;
@@ -1914,7 +2180,7 @@ dsi_status dsi_kv_set_length(dsi_kv* kv, int32_t window, int32_t len) {
   if (!kv) return fail(DSI_EINVAL, "null kv");
   if (window < 0 || window >= kv->n_windows || len < 0 || len > kv->max_len)
     return fail(DSI_EINVAL, "bad window / len");
-  HIP_TRY(launch_kv_set(kv->lens, window, len, kv->m->stream));
+  HIP_TRY(launch_kv_set(kv->forks(), window, len, kv->m->stream));
   kv->hi[window] = kv->lo[window] = len;
   return DSI_OK;
 }

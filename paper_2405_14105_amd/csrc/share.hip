@@ -1,0 +1,546 @@
+// Windows that continue one prompt: forking a window's cache into others, and
+// attention that reads the prefix they share once for all of them.
+//
+// Attention of row i of window b (position L_b + i) over keys [0, L_b + i] is
+// split at s, the largest multiple of 32 up to which every window of a group
+// holds what the window they were forked from holds.  Softmax sums over
+// disjoint keys join exactly: with (m, l, O) = (max, sum of e^(z - m), sum of
+// e^(z - m) v) of each part,
+//   M = max m_c,  out = sum_c e^(m_c - M) O_c / sum_c e^(m_c - M) l_c.
+// The keys [0, s) are every row's, so the B R rows of a group are one product
+// without a mask, over one copy of the prefix; the rest is each window's own.
+// One launch runs both kinds of part, a second joins them.
+#include <limits.h>
+#include <math.h>
+
+#include "scan.h"
+
+namespace dsi {
+
+namespace {
+
+constexpr int SW = 8;                  // waves per workgroup
+constexpr int kMinShared = 128;        // a shorter shared prefix is read by each window
+constexpr int kMinPrefixChunk = 256;   // keys per workgroup at least
+constexpr int kTailChunk = SW * 32;    // keys of a window's own per workgroup: a multiple of this
+
+__device__ __forceinline__ int wave_min(int v) {
+  dpp_steps([&](auto s) { v = min(v, dpp_from<decltype(s)::ctrl, decltype(s)::rows>(v, v)); });
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
+// positions of the prefix that the group's windows share, whole blocks of 32
+// (each wave finds it for itself)
+__device__ __forceinline__ int group_prefix(const ShareArgs& a, const ShareGroup& g) {
+  int s = a.maxlen;
+  for (int i = threadIdx.x & 63; i < g.count; i += 64) {
+    const int w = a.window0 + g.first + i;
+    int x = a.f.lens[w];
+    if (w != g.root) x = a.f.root[w] == g.root ? min(x, a.f.shared[w]) : 0;
+    s = min(s, x);
+  }
+  s = wave_min(s) & ~31;
+  return s < kMinShared ? 0 : s;
+}
+__device__ __forceinline__ int window_prefix(const ShareArgs& a, int win) {
+  for (int g = 0; g < a.n_groups; ++g)
+    if (win >= a.group[g].first && win < a.group[g].first + a.group[g].count) return group_prefix(a, a.group[g]);
+  return 0;
+}
+// keys per chunk: at most `most` chunks
+__device__ __forceinline__ int prefix_chunk(int s, int most) {
+  return max(kMinPrefixChunk, ((s + most - 1) / most + 63) & ~63);
+}
+__device__ __forceinline__ int tail_chunk(int keys, int most) {
+  return ((keys + most - 1) / most + kTailChunk - 1) / kTailChunk * kTailChunk;
+}
+
+// Queries of one part: `rows` consecutive rows from row0 on, times the G query
+// heads of KV head kvh; query q is row q % rows of head q / rows.
+struct QuerySet {
+  int row0, rows, kvh;
+};
+// Keys [k0, k1) of cache window `win`.  Those from `own` on are the rows of
+// the call: key own + j is seen by rows i >= j of the window (tree: by those
+// that have bit j).
+struct KeyRange {
+  int win, k0, k1, own;
+};
+
+// One part on the direct path: 16 queries, eight waves that take every eighth
+// 32-key step, keys and values straight from the cache into fragments (as in
+// the window attention: 16x16 MFMAs, S^T = K Q^T and O^T += V^T P^T, queries
+// and probabilities of a bf16 cache as hi + lo).  The waves' sums are joined in
+// LDS and leave as chunk `slot` of the partials.
+template <int KVB, int HD>
+__device__ void direct_part(const ShareArgs& a, const QuerySet& qs, const KeyRange& ks, int y, int slot, char* lds) {
+  constexpr int DS = HD / 32, DT = HD / 16;
+  float(*sm)[16] = (float(*)[16])lds;
+  float(*sl)[16] = (float(*)[16])(lds + SW * 16 * 4);
+  f32x4(*so)[DT][64] = (f32x4(*)[DT][64])(lds + 2 * SW * 16 * 4);
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = a.n_heads / a.n_kv, r16 = lane & 15, kgrp = (lane >> 4) * 8;
+  const int qn = G * qs.rows;
+  const int qi = y * 16 + r16;
+  const bool qvalid = qi < qn;
+  const int gh = qvalid ? qi / qs.rows : 0, ri = qvalid ? qi % qs.rows : 0;
+  const int m = qs.row0 + ri, head = qs.kvh * G + gh;
+  const int qpos = !qvalid ? -1 : ks.own == INT_MAX ? INT_MAX : ks.own + ri;
+  const unsigned long long anc = a.anc && qvalid && ks.own != INT_MAX ? a.anc[m] : ~0ull;
+  const size_t base = ((size_t)ks.win * a.n_kv + qs.kvh) * (size_t)a.maxlen * HD;
+  const float scale2 = a.scale * 1.44269504088896340736f;   // log2 e
+
+  struct KV16 {
+    u32x4 k[2][DS], v[DT];
+  };
+  struct KV32 {
+    F8 k[2][DS], v[DT];
+  };
+  KV16 b16;
+  KV32 b32;
+  auto load_k = [&](int p0) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int key = p0 + (r16 >> 2) * 8 + t * 4 + (r16 & 3);
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds) {
+        const size_t i = base + kc_off(key, ds * 32 + kgrp, HD);
+        if (KVB) {
+          b16.k[t][ds] = *(const u32x4*)((const uint16_t*)a.kc + i);
+        } else {
+          b32.k[t][ds].a = *(const float4*)((const float*)a.kc + i);
+          b32.k[t][ds].b = *(const float4*)((const float*)a.kc + i + 4);
+        }
+      }
+    }
+  };
+  auto load_v = [&](int p0) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      const size_t i = base + vc_off(p0 + kgrp, t * 16 + r16, HD);
+      if (KVB) {
+        b16.v[t] = *(const u32x4*)((const uint16_t*)a.vc + i);
+      } else {
+        b32.v[t].a = *(const float4*)((const float*)a.vc + i);
+        b32.v[t].b = *(const float4*)((const float*)a.vc + i + 4);
+      }
+    }
+  };
+  const float* qrow = a.q + (size_t)m * (a.n_heads * HD) + head * HD;
+  F8 qf[DS];
+#pragma unroll
+  for (int ds = 0; ds < DS; ++ds) {
+    qf[ds].a = qvalid ? *(const float4*)(qrow + ds * 32 + kgrp) : float4{0.f, 0.f, 0.f, 0.f};
+    qf[ds].b = qvalid ? *(const float4*)(qrow + ds * 32 + kgrp + 4) : float4{0.f, 0.f, 0.f, 0.f};
+  }
+  bf16x8 qh[DS], ql[DS];
+  if (KVB) {
+#pragma unroll
+    for (int ds = 0; ds < DS; ++ds) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = f8_get(qf[ds], e);
+      u32x4 h, l;
+      split8(v, h, l);
+      qh[ds] = as_bf16x8(h);
+      ql[ds] = as_bf16x8(l);
+    }
+  }
+  float mrun = -INFINITY, lrun = 0.f;
+  f32x4 o[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // the first loads of a wave without keys (its step lies past k1) are of the
+  // part's first keys and not used: registers that are loaded on one path only
+  // are not left to the compiler
+  int p0 = ks.k0 + 32 * w;
+  load_k(p0 < ks.k1 ? p0 : ks.k0);
+  load_v(p0 < ks.k1 ? p0 : ks.k0);
+  for (; p0 < ks.k1; p0 += 32 * SW) {
+    const int pn = p0 + 32 * SW;
+    f32x4 st[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      st[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds) {
+        if (KVB) {
+          const bf16x8 kb = as_bf16x8(b16.k[t][ds]);
+          st[t] = mfma_bf16(kb, qh[ds], st[t]);
+          st[t] = mfma_bf16(kb, ql[ds], st[t]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) st[t] = mfma_f32(f8_get(b32.k[t][ds], e), f8_get(qf[ds], e), st[t]);
+        }
+      }
+    }
+    if (pn < ks.k1) load_k(pn);
+    // lane: keys p0 + kgrp + e of query r16, base-2 units
+    const bool full = p0 + 32 <= ks.k1 && (ks.own == INT_MAX || p0 + 32 <= ks.own);
+    float pv[8];
+    unsigned seen = 0xFF;
+    float mloc = -INFINITY;
+    if (!full) {
+      seen = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int key = p0 + kgrp + e;
+        bool vis = key <= qpos && key < ks.k1;
+        vis = vis && (key < ks.own || ((anc >> ((key - ks.own) & 63)) & 1ull));
+        seen |= vis ? 1u << e : 0u;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      pv[e] = seen >> e & 1 ? st[e >> 2][e & 3] * scale2 : -INFINITY;
+      mloc = fmaxf(mloc, pv[e]);
+    }
+    mloc = max_over_16_32(mloc);
+    const float mnew = fmaxf(mrun, mloc);
+    const float b = mnew == -INFINITY ? 0.f : mnew;
+    float lsum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      pv[e] = __builtin_amdgcn_exp2f(pv[e] - b);
+      lsum += pv[e];
+    }
+    if (__ballot(mnew != mrun)) {
+      const float alpha = __builtin_amdgcn_exp2f(mrun - b);
+      lrun *= alpha;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) o[t] *= alpha;
+    }
+    lrun += lsum;
+    mrun = mnew;
+    // A step that some query does not see whole: values past k1 are dead cache
+    // rows and become 0, whatever they hold.  A value of the call's rows that
+    // is not finite would reach the rows before it as 0 * inf: it becomes 0 as
+    // well, and joins the rows that see it one by one.
+    if (!full) {
+      const int nv = ks.k1 - (p0 + kgrp);
+      bool odd = false;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        if (KVB) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t x = b16.v[t][i] & ((2 * i < nv ? 0x0000FFFFu : 0u) | (2 * i + 1 < nv ? 0xFFFF0000u : 0u));
+            const bool lo = (x & 0x7F80u) == 0x7F80u, hi = (x & 0x7F800000u) == 0x7F800000u;
+            odd |= lo || hi;
+            x &= (lo ? 0u : 0x0000FFFFu) | (hi ? 0u : 0xFFFF0000u);
+            b16.v[t][i] = x;
+          }
+        } else {
+          float x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x[e] = e < nv ? f8_get(b32.v[t], e) : 0.f;
+            const bool bad = !(fabsf(x[e]) < INFINITY);
+            odd |= bad;
+            x[e] = bad ? 0.f : x[e];
+          }
+          b32.v[t].a = float4{x[0], x[1], x[2], x[3]};
+          b32.v[t].b = float4{x[4], x[5], x[6], x[7]};
+        }
+      }
+      if (__ballot(odd)) {
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float p = __shfl(pv[e], r16 + 16 * g);
+            const unsigned vis = __shfl(seen, r16 + 16 * g);
+            const int key = p0 + 8 * g + e;
+            if (!(vis >> e & 1)) continue;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const size_t i = base + vc_off(key, t * 16 + (lane >> 4) * 4 + j, HD);
+                const float v = KVB ? bf_bits2f(((const uint16_t*)a.vc)[i]) : ((const float*)a.vc)[i];
+                if (!(fabsf(v) < INFINITY)) o[t][j] += p * v;
+              }
+          }
+      }
+    }
+    if (KVB) {
+      u32x4 h, l;
+      split8(pv, h, l);
+      const bf16x8 ph = as_bf16x8(h), pl = as_bf16x8(l);
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        const bf16x8 vv = as_bf16x8(b16.v[t]);
+        o[t] = mfma_bf16(vv, ph, o[t]);
+        o[t] = mfma_bf16(vv, pl, o[t]);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[t] = mfma_f32(f8_get(b32.v[t], e), pv[e], o[t]);
+    }
+    if (pn < ks.k1) load_v(pn);
+  }
+
+  lrun = sum_over_16_32(lrun);
+  if (lane < 16) {
+    sm[w][lane] = mrun;
+    sl[w][lane] = lrun;
+  }
+#pragma unroll
+  for (int t = 0; t < DT; ++t) so[w][t][lane] = o[t];
+  __syncthreads();
+  const size_t row = (size_t)slot * a.B * a.R * a.n_heads;
+  for (int it = threadIdx.x; it < DT * 64; it += SW * 64) {
+    const int t = it >> 6, l = it & 63, q = l & 15, qc = y * 16 + q;
+    if (qc >= qn) continue;
+    float M = sm[0][q];
+#pragma unroll
+    for (int x = 1; x < SW; ++x) M = fmaxf(M, sm[x][q]);
+    const float b = M == -INFINITY ? 0.f : M;
+    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    float L = 0.f;
+#pragma unroll
+    for (int x = 0; x < SW; ++x) {
+      const float f = __builtin_amdgcn_exp2f(sm[x][q] - b);
+      acc += so[x][t][l] * f;
+      L += sl[x][q] * f;
+    }
+    const size_t r = row + (size_t)(qs.row0 + qc % qs.rows) * a.n_heads + qs.kvh * G + qc / qs.rows;
+    *(f32x4*)(a.part_o + r * HD + t * 16 + (l >> 4) * 4) = acc;
+    if (t == 0 && l < 16) a.part_ml[r] = make_float2(M, L);
+  }
+}
+
+template <int KVB, int HD>
+__global__ __launch_bounds__(SW * 64) void k_share(ShareArgs a) {
+  __shared__ __align__(16) char lds[2 * SW * 16 * 4 + SW * HD * 64];
+  // ids of one KV head are equal mod n_kv: with eight or a multiple of eight
+  // KV heads, the parts that read the same keys run on one XCD
+  const int n_prefix = a.n_groups * a.n_kv * a.p_tiles * a.p_chunks;
+  int id = blockIdx.x;
+  if (id < n_prefix) {
+    const int kvh = id % a.n_kv;
+    id /= a.n_kv;
+    const ShareGroup& g = a.group[id % a.n_groups];
+    id /= a.n_groups;
+    const int y = id % a.p_tiles, c = id / a.p_tiles;
+    const int s = group_prefix(a, g), per = prefix_chunk(s, a.p_chunks);
+    const QuerySet qs{g.first * a.R, g.count * a.R, kvh};
+    if (c * per >= s || y * 16 >= qs.rows * (a.n_heads / a.n_kv)) return;
+    direct_part<KVB, HD>(a, qs, KeyRange{g.root, c * per, min(s, c * per + per), INT_MAX}, y, c, lds);
+    return;
+  }
+  id -= n_prefix;
+  const int kvh = id % a.n_kv;
+  id /= a.n_kv;
+  const int win = id % a.B;
+  id /= a.B;
+  const int y = id % a.t_tiles, c = id / a.t_tiles;
+  const int s = window_prefix(a, win);
+  const int len = min(a.f.lens[a.window0 + win], a.maxlen - a.R);
+  const int keys = len + a.R - s, per = tail_chunk(keys, a.t_chunks);
+  if (c * per >= keys) return;
+  direct_part<KVB, HD>(a, QuerySet{win * a.R, a.R, kvh},
+                       KeyRange{a.window0 + win, s + c * per, min(len + a.R, s + c * per + per), len}, y, a.p_chunks + c,
+                       lds);
+}
+
+// Joins the parts of every (row, head), in order: one workgroup per row and 256
+// pieces of four dims.
+template <int HD>
+__global__ __launch_bounds__(256) void k_share_join(ShareArgs a) {
+  const int m = blockIdx.x, win = m / a.R;
+  const int i = blockIdx.y * 256 + threadIdx.x;
+  const int s = window_prefix(a, win);
+  const int keys = min(a.f.lens[a.window0 + win], a.maxlen - a.R) + a.R - s;
+  const int np = s ? (s + prefix_chunk(s, a.p_chunks) - 1) / prefix_chunk(s, a.p_chunks) : 0;
+  const int nt = (keys + tail_chunk(keys, a.t_chunks) - 1) / tail_chunk(keys, a.t_chunks);
+  if (i >= a.n_heads * HD / 4) return;
+  const int head = i / (HD / 4), d = i % (HD / 4) * 4;
+  const size_t rows = (size_t)a.B * a.R * a.n_heads, r = (size_t)m * a.n_heads + head;
+  constexpr int CB = 8;
+  float M = -INFINITY, base = 0.f, L = 0.f;
+  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int c0 = 0; c0 < np + nt; c0 += CB) {
+    float2 ml[CB];
+    f32x4 o[CB];
+#pragma unroll
+    for (int j = 0; j < CB; ++j)
+      if (c0 + j < np + nt) {
+        const size_t slot = (size_t)(c0 + j < np ? c0 + j : a.p_chunks + c0 + j - np) * rows + r;
+        ml[j] = a.part_ml[slot];
+        o[j] = *(const f32x4*)(a.part_o + slot * HD + d);
+      }
+#pragma unroll
+    for (int j = 0; j < CB; ++j)
+      if (c0 + j < np + nt) M = fmaxf(M, ml[j].x);
+    const float b = M == -INFINITY ? 0.f : M;
+    if (c0) {
+      const float f = __builtin_amdgcn_exp2f(base - b);
+      L *= f;
+      acc *= f;
+    }
+    base = b;
+#pragma unroll
+    for (int j = 0; j < CB; ++j)
+      if (c0 + j < np + nt) {
+        const float f = __builtin_amdgcn_exp2f(ml[j].x - b);
+        L += ml[j].y * f;
+        acc += o[j] * f;
+      }
+  }
+  const float inv = 1.0f / L;
+  const float y4[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+  if (a.out_rows) *(float4*)(a.out_rows + r * HD + d) = float4{y4[0], y4[1], y4[2], y4[3]};
+  else pack_store4(a.out, a.wtype, m, head * HD + d, y4);
+}
+
+template <int KVB, int HD>
+hipError_t launch_shared_hd(const ShareArgs& a, hipStream_t s) {
+  const long long wgs = (long long)a.n_groups * a.n_kv * a.p_tiles * a.p_chunks + (long long)a.B * a.n_kv * a.t_tiles * a.t_chunks;
+  if (wgs > INT_MAX) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((k_share<KVB, HD>), dim3((unsigned)wgs), dim3(SW * 64), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_share_join<HD>), dim3(a.B * a.R, (a.n_heads * HD / 4 + 255) / 256), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+// one workgroup per row: its keys and values, rounded to the cache's type, into
+// slot L_b + i
+template <typename T>
+__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
+  const int m = blockIdx.x, win = a.window0 + m / a.R;
+  const int p = a.lens[win] + m % a.R;
+  if (p >= a.maxlen) return;
+  const int n = a.n_kv * a.hd;
+  auto put = [](T* dst, float x) {
+    if constexpr (sizeof(T) == 2) *dst = f2bf_bits(x);
+    else *dst = x;
+  };
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const size_t base = ((size_t)win * a.n_kv + i / a.hd) * (size_t)a.maxlen * a.hd;
+    put((T*)a.kc + base + kc_off(p, i % a.hd, a.hd), a.k[(size_t)m * n + i]);
+    put((T*)a.vc + base + vc_off(p, i % a.hd, a.hd), a.v[(size_t)m * n + i]);
+  }
+}
+
+__global__ void k_kv_advance(int* lens, int window0, int B, int rows) {
+  for (int b = threadIdx.x; b < B; b += blockDim.x) lens[window0 + b] += rows;
+}
+
+__global__ void k_fork_cut(ForkState f, int window, int new_len) { fork_cut(f, window, new_len); }
+
+// Copies positions [0, len) of window src into n windows: one workgroup per
+// 32-position block of a (layer, KV head), which holds its keys and values in
+// registers and stores them n times.  The positions behind len in its last
+// block stay as they are in the windows.  The first workgroup sets the lengths
+// and the record of what is shared: nothing else of this launch reads those.
+template <int ESZ>
+__global__ __launch_bounds__(256) void k_kv_fork(ForkArgs a) {
+  const int have = a.f.lens[a.src];
+  const int len = a.len < 0 ? have : a.len;
+  const bool first = blockIdx.x == 0 && blockIdx.y == 0;
+  const bool bad = len > have;
+  constexpr int VE = 16 / ESZ;           // elements per 16 bytes
+  constexpr int MOST = 128 * 32 / VE / 256;   // 16-byte pieces per thread of a block's keys (and values)
+  const int pieces = a.hd * 32 / VE;
+  const int layer = blockIdx.y / a.n_kv, h = blockIdx.y % a.n_kv;
+  const size_t head = (size_t)h * a.maxlen * a.hd * ESZ;
+  char* kc = (char*)a.kc + layer * a.layer_bytes + head;
+  char* vc = (char*)a.vc + layer * a.layer_bytes + head;
+  for (int blk = blockIdx.x; blk * 32 < len && !bad; blk += gridDim.x) {
+    const size_t at = (size_t)blk * 32 * a.hd * ESZ;
+    const int live = min(32, len - blk * 32);
+    u32x4 k[MOST], v[MOST];
+#pragma unroll
+    for (int i = 0; i < MOST; ++i) {
+      const int p = i * 256 + threadIdx.x;
+      if (p < pieces) {
+        k[i] = ((const u32x4*)(kc + a.src * a.win_bytes + at))[p];
+        v[i] = ((const u32x4*)(vc + a.src * a.win_bytes + at))[p];
+      }
+    }
+    for (int w = a.window0; w < a.window0 + a.n; ++w) {
+      u32x4* dk = (u32x4*)(kc + w * a.win_bytes + at);
+      u32x4* dv = (u32x4*)(vc + w * a.win_bytes + at);
+#pragma unroll
+      for (int i = 0; i < MOST; ++i) {
+        const int p = i * 256 + threadIdx.x;
+        if (p >= pieces) continue;
+        if (live == 32) {
+          dk[p] = k[i];
+          dv[p] = v[i];
+        } else {
+          // a piece of keys is VE dims of one position, one of values VE positions of one dim
+          if (p * VE / 32 % 32 < live) dk[p] = k[i];
+          const int p0 = p * VE % 32;
+#pragma unroll
+          for (int e = 0; e < VE; ++e)
+            if (p0 + e < live) {
+              if constexpr (ESZ == 2) ((uint16_t*)(dv + p))[e] = (uint16_t)(v[i][e / 2] >> (e % 2 * 16));
+              else ((uint32_t*)(dv + p))[e] = v[i][e];
+            }
+        }
+      }
+    }
+  }
+  if (!first) return;
+  if (bad && threadIdx.x == 0) atomicOr(a.err, 16);
+  // what other windows shared with the overwritten ones ends
+  for (int w = threadIdx.x; w < a.f.n_windows; w += 256) {
+    const bool into = w >= a.window0 && w < a.window0 + a.n;
+    if (into) {
+      a.f.lens[w] = bad ? 0 : len;
+      a.f.root[w] = a.src;
+      a.f.shared[w] = bad ? 0 : len;
+    } else if (a.f.root[w] >= a.window0 && a.f.root[w] < a.window0 + a.n) {
+      a.f.shared[w] = 0;
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_attention_shared(int kv_bf16, int hd, const ShareArgs& a, hipStream_t s) {
+  if (a.B < 1 || a.R < 1 || a.t_tiles < 1 || a.t_chunks < 1 || a.n_groups < 0 || a.n_groups > kMaxForkGroups ||
+      (a.n_groups && (a.p_tiles < 1 || a.p_chunks < 1)) || a.p_chunks < 0)
+    return hipErrorInvalidValue;
+  switch (hd) {
+    case 32: return kv_bf16 ? launch_shared_hd<1, 32>(a, s) : launch_shared_hd<0, 32>(a, s);
+    case 64: return kv_bf16 ? launch_shared_hd<1, 64>(a, s) : launch_shared_hd<0, 64>(a, s);
+    case 96: return kv_bf16 ? launch_shared_hd<1, 96>(a, s) : launch_shared_hd<0, 96>(a, s);
+    case 128: return kv_bf16 ? launch_shared_hd<1, 128>(a, s) : launch_shared_hd<0, 128>(a, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_kv_append(const AppendArgs& a, hipStream_t s) {
+  if (a.B < 1 || a.R < 1) return hipErrorInvalidValue;
+  if (a.kv_bf16) hipLaunchKernelGGL((k_kv_append<uint16_t>), dim3(a.B * a.R), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_kv_append<float>), dim3(a.B * a.R), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_advance(int* lens, int window0, int B, int rows, hipStream_t s) {
+  hipLaunchKernelGGL(k_kv_advance, dim3(1), dim3(64), 0, s, lens, window0, B, rows);
+  return hipGetLastError();
+}
+
+hipError_t launch_fork_cut(const ForkState& f, int window, int new_len, hipStream_t s) {
+  hipLaunchKernelGGL(k_fork_cut, dim3(1), dim3(64), 0, s, f, window, new_len);
+  return hipGetLastError();
+}
+
+// max_len: a bound on the positions taken, for the grid only
+hipError_t launch_kv_fork(const ForkArgs& a, int max_len, hipStream_t s) {
+  if (a.n < 1 || a.hd % 32 || a.hd > 128) return hipErrorInvalidValue;
+  const dim3 grid(max_len > 32 ? (max_len + 31) / 32 : 1, a.n_layers * a.n_kv);
+  if (a.esz == 2) hipLaunchKernelGGL((k_kv_fork<2>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_kv_fork<4>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace dsi

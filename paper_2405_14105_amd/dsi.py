@@ -19,6 +19,8 @@ DSI_OK, DSI_EINVAL, DSI_ENOMEM, DSI_EHIP, DSI_ECAPACITY, DSI_ESTATE = range(6)
 DSI_F32, DSI_BF16 = 0, 1
 DSI_SAMPLE, DSI_GREEDY = 0, 1
 DSI_MAX_ROWS = 64
+DSI_MAX_ATTEND_ROWS = 1024
+DSI_MAX_TOP = 64
 TENSOR_IDS = {
     "embed": 0, "final_norm": 1, "lm_head": 2, "attn_norm": 3, "wq": 4, "wk": 5, "wv": 6,
     "wo": 7, "ffn_norm": 8, "w_gate": 9, "w_up": 10, "w_down": 11,
@@ -26,8 +28,8 @@ TENSOR_IDS = {
 EXPORTED = (
     "dsi_model_create", "dsi_model_set_tensor", "dsi_model_destroy", "dsi_kv_create",
     "dsi_kv_destroy", "dsi_prefill", "dsi_verify", "dsi_verify_tree", "dsi_draft", "dsi_accept",
-    "dsi_accept_noalloc",
-    "dsi_kv_rollback", "dsi_kv_poison", "dsi_kv_length", "dsi_sync", "dsi_kv_export", "dsi_kv_import", "dsi_kv_set_length",
+    "dsi_accept_noalloc", "dsi_kv_bytes", "dsi_kv_wrap", "dsi_kv_fork", "dsi_attend", "dsi_logprobs_workspace",
+    "dsi_logprobs", "dsi_kv_rollback", "dsi_kv_poison", "dsi_kv_length", "dsi_sync", "dsi_kv_export", "dsi_kv_import", "dsi_kv_set_length",
     "dsi_profile_begin", "dsi_profile_end", "dsi_profile_kernel", "dsi_profile_stream", "dsi_last_error",
 )
 DSI_K_QKV, DSI_K_ATTN, DSI_K_OPROJ, DSI_K_GATEUP, DSI_K_DOWN, DSI_K_HEAD, DSI_K_VERIFY = range(1, 8)
@@ -65,6 +67,24 @@ class dsi_tree_args(ctypes.Structure):
     ]
 
 
+class dsi_attend_args(ctypes.Structure):
+    _fields_ = [
+        ("layer", ctypes.c_int32), ("window0", ctypes.c_int32), ("n_windows", ctypes.c_int32),
+        ("rows", ctypes.c_int32), ("d_q", ctypes.c_void_p), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
+        ("commit", ctypes.c_int32), ("d_out", ctypes.c_void_p),
+    ]
+
+
+class dsi_logprobs_args(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("n_top", ctypes.c_int32),
+        ("ld", ctypes.c_int64), ("d_logits", ctypes.c_void_p), ("d_targets", ctypes.c_void_p),
+        ("temperature", ctypes.c_float), ("d_logprob", ctypes.c_void_p), ("d_entropy", ctypes.c_void_p),
+        ("d_top_ids", ctypes.c_void_p), ("d_top_logprobs", ctypes.c_void_p), ("d_ws", ctypes.c_void_p),
+        ("ws_bytes", ctypes.c_size_t),
+    ]
+
+
 _lib = None
 
 
@@ -90,6 +110,12 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "dsi_draft": ([P, P, I32, P, I32, I32, P, F, P, P], I32),
         "dsi_accept": ([P, I32, I32, I32, P, P, P, P, F, I32, P, P], I32),
         "dsi_accept_noalloc": ([P, I32, I32, I32, P, P, P, P, F, I32, P, P], I32),
+        "dsi_kv_bytes": ([P, I32, I32, ctypes.POINTER(SZ)], I32),
+        "dsi_kv_wrap": ([P, I32, I32, P, P, SZ, PP], I32),
+        "dsi_kv_fork": ([P, I32, I32, I32, I32], I32),
+        "dsi_attend": ([P, P, ctypes.POINTER(dsi_attend_args)], I32),
+        "dsi_logprobs_workspace": ([I32, I32, I32, ctypes.POINTER(SZ)], I32),
+        "dsi_logprobs": ([P, ctypes.POINTER(dsi_logprobs_args)], I32),
         "dsi_kv_rollback": ([P, I32, I32], I32),
         "dsi_kv_poison": ([P, I32], I32),
         "dsi_kv_length": ([P, I32, ctypes.POINTER(ctypes.c_int32)], I32),
@@ -194,6 +220,44 @@ def dsi_accept_noalloc(stream: int, n_windows: int, k: int, vocab: int, d_logits
     _check(load().dsi_accept_noalloc(stream or None, n_windows, k, vocab, _ptr(d_logits), _ptr(d_tokens),
                                      _ptr(d_q), _ptr(d_u), temperature, mode, _ptr(d_n_accepted),
                                      _ptr(d_next_token)))
+
+
+def dsi_kv_bytes(model: int, n_windows: int, max_len: int) -> int:
+    """Bytes of such a cache's keys (and of its values)."""
+    out = ctypes.c_size_t()
+    _check(load().dsi_kv_bytes(model, n_windows, max_len, ctypes.byref(out)))
+    return out.value
+
+
+def dsi_kv_wrap(model: int, n_windows: int, max_len: int, d_k, d_v, nbytes: int) -> int:
+    out = ctypes.c_void_p()
+    _check(load().dsi_kv_wrap(model, n_windows, max_len, _ptr(d_k), _ptr(d_v), nbytes, ctypes.byref(out)))
+    return out.value
+
+
+def dsi_kv_fork(kv: int, src: int, window0: int, n_windows: int, length: int = -1):
+    _check(load().dsi_kv_fork(kv, src, window0, n_windows, length))
+
+
+def dsi_attend(model: int, kv: int, layer: int, window0: int, n_windows: int, rows: int, d_q, d_k, d_v, d_out,
+               commit: bool = False):
+    a = dsi_attend_args(layer, window0, n_windows, rows, _ptr(d_q), _ptr(d_k), _ptr(d_v), int(commit), _ptr(d_out))
+    _check(load().dsi_attend(model, kv, ctypes.byref(a)))
+
+
+def dsi_logprobs_workspace(rows: int, vocab: int, n_top: int) -> int:
+    """Bytes of the workspace that dsi_logprobs needs for these sizes."""
+    out = ctypes.c_size_t()
+    _check(load().dsi_logprobs_workspace(rows, vocab, n_top, ctypes.byref(out)))
+    return out.value
+
+
+def dsi_logprobs(stream: int, rows: int, vocab: int, d_logits, d_targets, n_top: int, d_logprob, d_entropy, d_top_ids,
+                 d_top_logprobs, d_ws, ws_bytes: int, temperature: float = 1.0, dtype: int = DSI_F32, ld: int = 0):
+    """ld: entries from one row of logits to the next (0: vocab)."""
+    a = dsi_logprobs_args(rows, vocab, dtype, n_top, ld or vocab, _ptr(d_logits), _ptr(d_targets), temperature,
+                          _ptr(d_logprob), _ptr(d_entropy), _ptr(d_top_ids), _ptr(d_top_logprobs), _ptr(d_ws), ws_bytes)
+    _check(load().dsi_logprobs(stream or None, ctypes.byref(a)))
 
 
 def dsi_kv_rollback(kv: int, window: int, new_len: int):

@@ -1,0 +1,161 @@
+"""Host code of forking, dsi_attend and dsi_logprobs, without a GPU: refusals,
+what is launched and what is allocated, against a HIP runtime that runs
+nothing (see test_host_runtime.py)."""
+import ctypes
+
+import pytest
+
+from paper_2405_14105_amd import dsi
+from test_host_runtime import pytestmark, run, stub  # noqa: F401
+
+
+def test_fork_refusals(stub):
+    run(stub, '''
+    m = model(S.SHAPES["gqa_hd64"])
+    kv = dsi.dsi_kv_create(m, 5, 300)
+    dsi.dsi_prefill(m, kv, 1, P, 100, P)
+    def refused(*a):
+        hip.stub_clear()
+        try:
+            dsi.dsi_kv_fork(kv, *a)
+        except dsi.DsiError as e:
+            assert e.status == dsi.DSI_EINVAL
+            assert not launches()
+            return True
+        return False
+    for a in ((-1, 0, 1), (5, 0, 1), (1, -1, 2), (1, 2, 0), (1, 2, 4), (1, 0, 2), (1, 1, 1), (1, 2, 3, 101), (1, 2, 3, -2),
+              (1, 2, 2 ** 31 - 1), (1, 2 ** 31 - 1, 1)):
+        assert refused(*a), a
+    for a in ((1, 2, 3), (1, 0, 1, 0), (1, 2, 3, 100), (1, 4, 1, 33)):
+        assert not refused(*a), a
+        assert [k for k, _, _ in launches()] == ["k_kv_fork"]
+    # the host's bounds are the source's: what fits follows
+    dsi.dsi_kv_fork(kv, 1, 2, 1)
+    dsi.dsi_prefill(m, kv, 2, P, 200, P)
+    try:
+        dsi.dsi_prefill(m, kv, 2, P, 1, P)
+        assert False
+    except dsi.DsiError as e:
+        assert e.status == dsi.DSI_ECAPACITY
+    ''')
+
+
+def test_wrap_refusals_and_ownership(stub):
+    run(stub, '''
+    m = model(S.SHAPES["gqa_hd64"])
+    n = dsi.dsi_kv_bytes(m, 3, 100)
+    s = S.SHAPES["gqa_hd64"]
+    assert n == s.n_layers * 3 * s.n_kv_heads * 128 * s.head_dim * 2
+    for a in ((0, 100, P, P, n), (3, 0, P, P, n), (3, 100, None, P, n), (3, 100, P, None, n), (3, 100, P + 8, P, n),
+              (3, 100, P, P + 2, n), (3, 100, P, P, n - 1), (3, 100, P, P, n + 1)):
+        try:
+            dsi.dsi_kv_wrap(m, *a)
+            assert False, a
+        except dsi.DsiError as e:
+            assert e.status == dsi.DSI_EINVAL, a
+    used = hip.stub_in_use()
+    kv = dsi.dsi_kv_wrap(m, 3, 100, P, P, n)
+    try:
+        dsi.dsi_model_destroy(m)
+        assert False
+    except dsi.DsiError as e:
+        assert e.status == dsi.DSI_ESTATE
+    dsi.dsi_kv_destroy(kv)              # frees nothing of the caller's (the runtime aborts on an address it did not give)
+    assert hip.stub_in_use() == used
+    dsi.dsi_model_destroy(m)
+    assert hip.stub_in_use() == 0
+    ''')
+
+
+def test_attend_refusals(stub):
+    run(stub, '''
+    m = model(S.SHAPES["gqa_hd64"])
+    other = model(S.SHAPES["gqa_hd64"])
+    kv = dsi.dsi_kv_create(m, 4, 100)
+    ok = dict(layer=1, window0=0, n_windows=4, rows=3, d_q=P, d_k=P, d_v=P, d_out=P)
+    def status(mm=m, **change):
+        hip.stub_clear()
+        try:
+            dsi.dsi_attend(mm, kv, **{**ok, **change})
+        except dsi.DsiError as e:
+            assert not launches() and not hip.stub_mallocs()
+            return e.status
+        return 0
+    assert status(other) == dsi.DSI_EINVAL
+    for change in (dict(layer=-1), dict(layer=3), dict(n_windows=0), dict(rows=0), dict(rows=257), dict(n_windows=5), dict(window0=1),
+                   dict(window0=-1), dict(d_q=None), dict(d_k=None), dict(d_v=None), dict(d_out=None), dict(d_q=P + 4), dict(d_out=P + 8),
+                   dict(window0=2 ** 31 - 1), dict(n_windows=2 ** 31 - 1, rows=2 ** 31 - 1)):
+        assert status(**change) == dsi.DSI_EINVAL, change
+    assert status(rows=101, n_windows=1) == dsi.DSI_ECAPACITY
+    assert status() == 0 and status(rows=100) == 0
+    assert status(rows=60, commit=True) == 0
+    assert status(rows=41) == dsi.DSI_ECAPACITY and status(rows=40) == 0
+    # no weights are needed
+    bare = dsi.dsi_model_create(dsi.make_config(1, 32, 4, 2, 64, 32, 32), STREAM)
+    bkv = dsi.dsi_kv_create(bare, 1, 50)
+    dsi.dsi_attend(bare, bkv, 0, 0, 1, 2, P, P, P, P)
+    ''')
+
+
+def test_what_runs_and_what_is_allocated(stub):
+    """Windows that were not forked run as before; a step's buffers are allocated by its first call."""
+    run(stub, '''
+    m = model(S.SHAPES["tiny"])
+    kv = dsi.dsi_kv_create(m, 8, 2000)
+    for w in range(8):
+        dsi.dsi_prefill(m, kv, w, P, 300, P)
+    def names(f):
+        hip.stub_clear()
+        f()
+        return {k for k, _, _ in launches()}
+    dsi.dsi_profile_begin(m, dsi.DSI_K_ATTN)      # launches one by one, no recorded step
+    def verify(w0, n, k=3):
+        return names(lambda: dsi.dsi_verify(m, kv, w0, n, k, P, P, P, P, P, commit=False))
+    def tree(w0, n):
+        return names(lambda: dsi.dsi_verify_tree(m, kv, w0, n, 4, P, P, P, P, P, commit=False))
+    assert "k_attn" in verify(0, 8) and "k_share" not in verify(0, 8)
+    dsi.dsi_kv_fork(kv, 2, 3, 2)
+    for f in (verify, tree):
+        for w0, n in ((2, 3), (3, 2), (0, 8), (2, 2)):
+            assert "k_share" in f(w0, n) and "k_attn" not in f(w0, n), (w0, n)
+        for w0, n in ((0, 3), (4, 4), (2, 1), (4, 1)):
+            assert "k_attn" in f(w0, n) and "k_share" not in f(w0, n), (w0, n)
+    # a chain of forks: the later root goes with its own
+    dsi.dsi_kv_fork(kv, 4, 5, 1)
+    assert "k_share" in verify(4, 2)
+    attend = lambda rows, n=8: names(lambda: dsi.dsi_attend(m, kv, 0, 0, n, rows, P, P, P, P))
+    assert attend(20) == {"k_kv_append", "k_share", "k_share_join"}
+    for rows in (20, 1, 7):
+        attend(rows)
+        assert hip.stub_mallocs() == 0, rows
+    hip.stub_clear()
+    hip.stub_capture(1)
+    dsi.dsi_attend(m, kv, 0, 0, 8, 20, P, P, P, P)
+    dsi.dsi_kv_fork(kv, 0, 1, 2, 64)
+    hip.stub_capture(0)
+    assert hip.stub_refused() == 0 and hip.stub_mallocs() == 0
+    ''')
+
+
+def test_logprobs_refusals():
+    lib = dsi.load()
+    P = 4096
+    n = ctypes.c_size_t()
+    for a in ((-1, 100, 1), ((1 << 24) + 1, 100, 1), (1, 0, 0), (1, (1 << 30) + 1, 1), (1, 100, -1), (1, 100, 65), (1, 3, 4)):
+        assert lib.dsi_logprobs_workspace(*a, ctypes.byref(n)) == dsi.DSI_EINVAL, a
+    assert lib.dsi_logprobs_workspace(1, 10, 1, None) == dsi.DSI_EINVAL
+    assert dsi.dsi_logprobs_workspace(0, 10, 1) == 0
+    need = dsi.dsi_logprobs_workspace(5, 32000, 4)
+    # what a row needs does not grow as the call gets larger, beyond four waves a SIMD in all
+    assert dsi.dsi_logprobs_workspace(100000, 128256, 4) == 100000 * (24 + 32)
+    ok = dict(rows=5, vocab=32000, d_logits=P, d_targets=P, n_top=4, d_logprob=P, d_entropy=P, d_top_ids=P, d_top_logprobs=P,
+              d_ws=P, ws_bytes=need)
+    for change in (dict(rows=-1), dict(vocab=0), dict(n_top=65), dict(n_top=-1), dict(dtype=2), dict(ld=31999), dict(ld=-5),
+                   dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=float("nan")), dict(temperature=float("inf")),
+                   dict(temperature=1e-39), dict(d_logits=None), dict(d_targets=None), dict(d_top_ids=None),
+                   dict(d_top_logprobs=None), dict(d_ws=None), dict(d_ws=P + 4), dict(ws_bytes=need - 1), dict(d_logits=P + 2),
+                   dict(dtype=dsi.DSI_BF16, d_logits=P + 1), dict(d_logprob=None, d_entropy=None, n_top=0)):
+        with pytest.raises(dsi.DsiError) as e:
+            dsi.dsi_logprobs(0, **{**ok, **change})
+        assert e.value.status == dsi.DSI_EINVAL, change
+    dsi.dsi_logprobs(0, **{**ok, "rows": 0, "d_logits": None, "d_ws": None, "ws_bytes": 0})
