@@ -394,7 +394,7 @@ struct LogprobArgs {
   // set by launch_logprobs
   int U;                // runs per row
   LpStat* stat;         // workspace [rows][U]
-  unsigned long long* keys;   // workspace [rows][U][n]
+  unsigned long long* keys;   // workspace [rows][n][U]
 };
 constexpr int kMaxTop = 64;
 constexpr int kMaxLogprobRows = 1 << 24, kMaxLogprobVocab = 1 << 30;
@@ -446,14 +446,16 @@ struct ShareArgs {
   const unsigned long long* anc;   // nullable: token-tree rows (AttnArgs)
   int n_groups;
   ShareGroup group[kMaxForkGroups];
-  int p_tiles, p_chunks;   // of a group's prefix: query tiles (16 rows x heads) and key chunks at most
-  int t_tiles, t_chunks;   // of a window's own keys
+  int p_tile;           // queries (rows x heads of one KV head) per workgroup of a prefix: share_tile
+  int p_tiles, p_chunks;   // of a group's prefix: query tiles and key chunks at most
+  int t_tiles, t_chunks;   // of a window's own keys: tiles of 16 queries
   float* part_o;        // [p_chunks + t_chunks][B * R * n_heads][hd]
   float2* part_ml;      // [p_chunks + t_chunks][B * R * n_heads]
   PackRef out;          // O-projection input pack, or
   int wtype;
   float* out_rows;      // [B * R][n_heads * hd] instead (nullable)
 };
+int share_tile(int kv_bf16, int queries);
 hipError_t launch_attention_shared(int kv_bf16, int hd, const ShareArgs& a, hipStream_t s);
 // rows' keys and values [B * R][n_kv * hd] into the cache behind each window's length
 struct AppendArgs {

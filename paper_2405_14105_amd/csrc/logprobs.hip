@@ -10,12 +10,14 @@
 // it moves: the 16 terms of a step are added in fp32, the steps in fp64.  The
 // entries equal to the maximum are counted, not summed, so that S - 1 of a
 // row that is sure of one token keeps its digits (log1p).
-// Alternatives: a wave keeps its n largest entries sorted across its lanes,
-// key = (logit in unsigned order, id complemented).  A step whose lanes hold
-// nothing above the n-th key costs one ballot; otherwise its largest entries
-// are taken one by one, so that no order of the entries makes a step insert
-// more than n times.  No wave waits for another.  A second launch, one wave a
-// row, joins the runs: statistics in fp64, and a merge of the U sorted lists.
+// Alternatives: a wave keeps its largest entries sorted across its lanes, key =
+// (logit in unsigned order, id complemented).  A step whose lanes hold nothing
+// above the n-th key costs one ballot.  Otherwise a few alternatives are taken
+// one by one, largest first; for more, the entries not below the n-th largest
+// lane maximum (n entries are at least that) are gathered in LDS, 64 at a time
+// sorted across the lanes and merged with the list.  No wave waits for another.
+// A second launch, one wave a row, joins the runs: statistics in fp64, and the
+// runs' lists, best ranks first, 64 keys at a time.
 // Bound by reading the logits where there are many rows, by the two launches
 // where there are few.
 #include <math.h>
@@ -29,8 +31,10 @@ namespace {
 constexpr int LPW = 4;                 // waves (runs) per workgroup of the first launch
 constexpr int LPE = 16;                // entries per lane and step
 constexpr int LPS = 64 * LPE;          // entries per step
-constexpr int LPG = 4;                 // lists per lane of the merge
+constexpr int LPG = 4;                 // runs per lane of the join
 constexpr int kLpRuns = 64 * LPG;      // runs per row at most
+// up to so many alternatives are taken one by one
+constexpr int kLpFew = 4;
 
 typedef unsigned long long u64;
 
@@ -53,6 +57,57 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
     v = v > o ? v : o;
   });
   return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+// the value of lane l ^ J, by lane swaps and DPP patterns (a shuffle goes
+// through LDS: a merge of 64 keys took 2 us by itself that way)
+template <int J>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v, int lane) {
+  const int x = (int)v;
+  if constexpr (J == 1) return (uint32_t)__builtin_amdgcn_update_dpp(x, x, 0xB1, 0xF, 0xF, false);
+  if constexpr (J == 2) return (uint32_t)__builtin_amdgcn_update_dpp(x, x, 0x4E, 0xF, 0xF, false);
+  if constexpr (J == 4) {   // 7 - l of eight lanes, then 3 - l of four
+    const int y = __builtin_amdgcn_update_dpp(x, x, 0x141, 0xF, 0xF, false);
+    return (uint32_t)__builtin_amdgcn_update_dpp(y, y, 0x1B, 0xF, 0xF, false);
+  }
+  if constexpr (J == 8) return (uint32_t)__builtin_amdgcn_update_dpp(x, x, 0x128, 0xF, 0xF, false);
+  if constexpr (J == 16) {
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return lane & 16 ? a[0] : a[1];
+  }
+  const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return lane & 32 ? a[0] : a[1];
+}
+template <int J>
+__device__ __forceinline__ u64 lane_xor(u64 v, int lane) {
+  return ((u64)lane_xor<J>((uint32_t)(v >> 32), lane) << 32) | lane_xor<J>((uint32_t)v, lane);
+}
+// Bitonic sort of 64 values across the lanes: in a sequence of size K, lane l
+// keeps the larger of the pair (l, l ^ J) when its bits K and J are equal (DOWN:
+// largest value first), or when they differ.
+constexpr u64 keep_larger(int k, int j, bool down) {   // a bit per lane
+  u64 m = 0;
+  for (int l = 0; l < 64; ++l)
+    if ((((l & k) == 0) == ((l & j) == 0)) == down) m |= 1ull << l;
+  return m;
+}
+template <int K, int J, bool DOWN, typename V>
+__device__ __forceinline__ void sort_steps(V& v, int lane) {
+  const V o = lane_xor<J>(v, lane);
+  constexpr u64 kLarger = keep_larger(K, J, DOWN);
+  const bool larger = __builtin_amdgcn_inverse_ballot_w64(kLarger);
+  v = (o > v) == larger ? o : v;
+  if constexpr (J > 1) sort_steps<K, J / 2, DOWN>(v, lane);
+}
+template <bool DOWN, int K = 2, typename V>
+__device__ __forceinline__ void wave_sort(V& v, int lane) {
+  sort_steps<K, K / 2, DOWN>(v, lane);
+  if constexpr (K < 64) wave_sort<DOWN, 2 * K>(v, lane);
+}
+// the 64 largest of a sorted list (largest first) and 64 keys in any order, sorted
+__device__ __forceinline__ void merge_keys(u64& list, u64 keys, int lane) {
+  wave_sort<false>(keys, lane);
+  list = list > keys ? list : keys;   // the larger ones, as a bitonic sequence
+  sort_steps<64, 32, true>(list, lane);
 }
 // the lane above takes this lane's value (wave_shr:1); lane 0 keeps its own
 __device__ __forceinline__ u64 from_lane_below(u64 v) {
@@ -114,7 +169,9 @@ __device__ __forceinline__ void load_step(Step<T>& s, const T* row, int a, int V
 
 template <typename T>
 __global__ __launch_bounds__(LPW * 64) void k_lp_rows(LogprobArgs a) {
+  __shared__ u64 gather[LPW][128];
   const int lane = threadIdx.x & 63;
+  u64* const held = gather[threadIdx.x >> 6];
   const int run = __builtin_amdgcn_readfirstlane(blockIdx.x * LPW + (threadIdx.x >> 6));
   if (run >= a.rows * a.U) return;
   const int r = run / a.U, u = run - r * a.U;
@@ -170,30 +227,65 @@ __global__ __launch_bounds__(LPW * 64) void k_lp_rows(LogprobArgs a) {
     t += (double)ts;
     if (a.n) {
       uint32_t bo = order_of(best);
-      while (__ballot(bo > tau)) {
-        const uint32_t mx = wave_umax(bo);
-        int idx = LPE;
+      if (!__ballot(bo > tau)) {
+      } else if (a.n <= kLpFew) {
+        uint32_t o[LPE];
 #pragma unroll
-        for (int i = LPE - 1; i >= 0; --i) idx = order_of(z[i]) == mx ? i : idx;
-        const uint32_t v = idx < LPE ? (uint32_t)(position<T>(st, lane, idx) - off) : ~0u;
-        // the lowest id among equals: the largest complement
-        const uint32_t nv = wave_umax(idx < LPE ? ~v : 0u);
-        const u64 key = ((u64)mx << 32) | nv;
-        const int pos = __popcll(__ballot(list > key));
-        const u64 below = from_lane_below(list);
-        list = lane > pos ? below : lane == pos ? key : list;
-        tau = (uint32_t)(lane_key(list, a.n - 1) >> 32);
-        // taken: out of the step
-        const bool mine = idx < LPE && ~v == nv;
-        best = -INFINITY;
-        uint32_t left = 0;
+        for (int i = 0; i < LPE; ++i) o[i] = order_of(z[i]);
+        do {
+          const uint32_t mx = wave_umax(bo);
+          int idx = LPE;
+#pragma unroll
+          for (int i = LPE - 1; i >= 0; --i) idx = o[i] == mx ? i : idx;
+          const uint32_t v = idx < LPE ? (uint32_t)(position<T>(st, lane, idx) - off) : ~0u;
+          // the lowest id among equals: the largest complement
+          const uint32_t nv = wave_umax(idx < LPE ? ~v : 0u);
+          const u64 key = ((u64)mx << 32) | nv;
+          const int pos = __popcll(__ballot(list > key));
+          const u64 below = from_lane_below(list);
+          list = lane > pos ? below : lane == pos ? key : list;
+          tau = (uint32_t)(lane_key(list, a.n - 1) >> 32);
+          // taken: out of the step
+          const bool mine = idx < LPE && ~v == nv;
+          bo = 0;
+#pragma unroll
+          for (int i = 0; i < LPE; ++i) {
+            o[i] = mine && i == idx ? 0u : o[i];
+            bo = bo > o[i] ? bo : o[i];
+          }
+        } while (__ballot(bo > tau));
+      } else {
+        // what equals the n-th key of the steps before has a larger id; within
+        // the step ids come in any order, and equals are kept
+        uint32_t o[LPE], s = bo;
+#pragma unroll
+        for (int i = 0; i < LPE; ++i) o[i] = order_of(z[i]);
+        wave_sort<true>(s, lane);
+        uint32_t bar = (uint32_t)__builtin_amdgcn_readlane((int)s, a.n - 1);
+        bar = bar > tau ? bar : tau + 1;
+        int have = 0;
 #pragma unroll
         for (int i = 0; i < LPE; ++i) {
-          z[i] = mine && i == idx ? NAN : z[i];
-          const uint32_t o = order_of(z[i]);
-          left = left > o ? left : o;
+          const bool in = o[i] >= bar;
+          const u64 mask = __ballot(in);
+          if (!mask) continue;
+          if (in) {
+            const int at = have + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+            held[at] = ((u64)o[i] << 32) | ~(uint32_t)(position<T>(st, lane, i) - off);
+          }
+          have += __popcll(mask);
+          if (have >= 64) {
+            merge_keys(list, held[lane], lane);
+            have -= 64;
+            if (lane < have) held[lane] = held[64 + lane];
+            tau = (uint32_t)(lane_key(list, a.n - 1) >> 32);
+            bar = bar > tau ? bar : tau;
+          }
         }
-        bo = left;
+        if (have) {
+          merge_keys(list, lane < have ? held[lane] : 0, lane);
+          tau = (uint32_t)(lane_key(list, a.n - 1) >> 32);
+        }
       }
     }
     cur = next;
@@ -210,7 +302,7 @@ __global__ __launch_bounds__(LPW * 64) void k_lp_rows(LogprobArgs a) {
   wt = wave_sum(wt);
   const double all = wave_sum(wc);
   if (lane == 0) a.stat[run] = LpStat{ws, wt, M, (float)all};
-  if (lane < a.n) a.keys[(size_t)run * a.n + lane] = list;
+  if (lane < a.n) a.keys[((size_t)r * a.n + lane) * a.U + u] = list;   // rank by rank
 }
 
 __global__ __launch_bounds__(64) void k_lp_join(LogprobArgs a) {
@@ -259,41 +351,29 @@ __global__ __launch_bounds__(64) void k_lp_join(LogprobArgs a) {
     }
   }
   if (!a.n) return;
-  // merge: each lane heads up to LPG sorted lists
-  const u64* keys = a.keys + (size_t)r * a.U * a.n;
-  u64 head[LPG];
-  int at[LPG];
-#pragma unroll
-  for (int j = 0; j < LPG; ++j) {
-    const int u = lane + 64 * j;
-    at[j] = 0;
-    head[j] = u < a.U ? keys[(size_t)u * a.n] : 0;
+  // the runs' keys, best ranks first: 64 at a time, the next ones in flight
+  const u64* keys = a.keys + (size_t)r * a.n * a.U;
+  const int total = a.n * a.U;
+  u64 list = 0, next = lane < total ? keys[lane] : 0;
+  u64 last = 0;   // the n-th key
+  for (int i0 = 0; i0 < total; i0 += 64) {
+    const u64 k = next;
+    next = i0 + 64 + lane < total ? keys[i0 + 64 + lane] : 0;
+    if (!__ballot(k > last)) continue;
+    merge_keys(list, k, lane);
+    last = lane_key(list, a.n - 1);
   }
-  for (int i = 0; i < a.n; ++i) {
-    u64 mine = head[0];
-#pragma unroll
-    for (int j = 1; j < LPG; ++j) mine = mine > head[j] ? mine : head[j];
-    const uint32_t hi = wave_umax((uint32_t)(mine >> 32));
-    const uint32_t lo = wave_umax((uint32_t)(mine >> 32) == hi ? (uint32_t)mine : 0u);
-    const u64 key = ((u64)hi << 32) | lo;
-    if (lane == 0) {
-      const size_t o = (size_t)r * a.n + i;
-      a.top_ids[o] = key ? (int)~lo : -1;
-      a.top_logprob[o] = key ? (float)(((double)from_order(hi) - (double)M) * a.inv_temperature - lse) : NAN;
-    }
-#pragma unroll
-    for (int j = 0; j < LPG; ++j)
-      if (key && head[j] == key) {
-        ++at[j];
-        head[j] = at[j] < a.n ? keys[(size_t)(lane + 64 * j) * a.n + at[j]] : 0;
-      }
+  if (lane < a.n) {
+    const size_t o = (size_t)r * a.n + lane;
+    a.top_ids[o] = list ? (int)~(uint32_t)list : -1;
+    a.top_logprob[o] = list ? (float)(((double)from_order((uint32_t)(list >> 32)) - (double)M) * a.inv_temperature - lse) : NAN;
   }
 }
 
 // Runs per row: about four waves a SIMD over the whole call, whole steps.
 int lp_runs(long long rows, int V) {
   const long long steps = ((long long)V + LPS - 1) / LPS;
-  long long u = (4096 + rows - 1) / rows;
+  long long u = (3072 + rows - 1) / rows;
   u = u < steps ? u : steps;
   return (int)(u < 1 ? 1 : u < kLpRuns ? u : kLpRuns);
 }

@@ -671,10 +671,11 @@ SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, 
     i += n;
   }
   const int G = m->hq / m->hkv;
+  a.p_tile = share_tile(m->kvb, G * R * most);
   a.t_tiles = cdiv(G * R, 16);
   a.t_chunks = std::min(std::max(1, 512 / (B * m->hkv * a.t_tiles)), cdiv(kv->max_len, 256));
   if (a.n_groups) {
-    a.p_tiles = cdiv(G * R * most, 16);
+    a.p_tiles = cdiv(G * R * most, a.p_tile);
     a.p_chunks = std::min(std::max(1, 256 / (a.n_groups * m->hkv * a.p_tiles)), cdiv(kv->max_len, 256));
   }
   p.parts = (size_t)(a.p_chunks + a.t_chunks) * B * R * m->hq;

@@ -313,9 +313,209 @@ __device__ void direct_part(const ShareArgs& a, const QuerySet& qs, const KeyRan
   }
 }
 
-template <int KVB, int HD>
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+__device__ __forceinline__ f32x16 mfma32_bf16(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// One part of a bf16 prefix for many queries: QT tiles of 32 queries, one a
+// wave, and KS = 8 / QT waves per tile that take the stage's 32-key blocks in
+// turn.  A stage's keys and values go through LDS once for all queries (two
+// stages, the next one's loads in flight in registers), so a CU takes in
+// HD * 128 bytes per 32 keys for 32 QT queries, and the matrix instructions
+// bound it from some 64 queries on.
+// 32x32x16 MFMAs, S^T[key][query] = K Q^T and O^T[dim][query] += V^T P^T: lane l
+// holds query l % 32 in all of them.  Row rho of S^T stands for key
+// 16 (j >> 1) + 8 h + 4 (j & 1) + i of the block, rho = 8 j + 4 h + i, so that
+// the 16 scores a lane gets are keys 16 c + 8 (l / 32) + 0..7, c = 0, 1: its
+// B operands of the second product.
+// A block of the cache is HD / 16 tiles of 1 KB for K (16 positions x 32 dims)
+// and for V (16 dims x 32 positions); 16-byte piece (row r, piece 2 c + h) of a
+// tile sits at c * 512 + h * 256 + r * 16 in LDS, so that every 16 lanes of a
+// fragment read 256 consecutive bytes.
+// Queries (times scale and log2 e) and probabilities are hi + lo bf16, as in
+// the window attention; the running maximum moves only when a score is 2^8 above
+// it, so most blocks rescale nothing.
+template <int HD, int QT>
+constexpr int tile_stage_blocks() { return SW / QT < 2 ? 2 : SW / QT; }
+template <int HD, int QT>
+constexpr int tile_lds() { return 2 * tile_stage_blocks<HD, QT>() * HD * 128 + SW * 32 * 8; }
+
+template <int HD, int QT>
+__device__ void tile_part(const ShareArgs& a, const QuerySet& qs, int win, int k0, int k1, int y, int slot, char* lds) {
+  constexpr int KS = SW / QT, SB = tile_stage_blocks<HD, QT>();
+  constexpr int TK = HD / 16, TB = 2 * TK, NPW = SB * TB / SW;
+  constexpr int DS = HD / 16, DT = HD / 32;
+  const int lane = threadIdx.x & 63, h = lane >> 5, c32 = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int qt = w % QT, ks = w / QT;
+  const int G = a.n_heads / a.n_kv, qn = G * qs.rows;
+  const int qi = (y * QT + qt) * 32 + c32;
+  const bool qvalid = qi < qn;
+  const int m = qs.row0 + (qvalid ? qi % qs.rows : 0), head = qs.kvh * G + (qvalid ? qi / qs.rows : 0);
+  const size_t base = ((size_t)win * a.n_kv + qs.kvh) * (size_t)a.maxlen * HD * 2;
+  const char* kc = (const char*)a.kc + base;
+  const char* vc = (const char*)a.vc + base;
+  const int blk0 = k0 >> 5, nblk = (k1 - k0) >> 5, stages = (nblk + SB - 1) / SB;
+  const int src = (lane & 15) * 64 + (lane >> 4) * 16;   // of this lane's piece in a tile
+
+  u32x4 sr[NPW];
+  auto load_stage = [&](int st) {
+#pragma unroll
+    for (int j = 0; j < NPW; ++j) {
+      const int i = w * NPW + j, tile = i % TB;
+      const size_t blk = (size_t)(blk0 + min(st * SB + i / TB, nblk - 1)) * (HD * 64);
+      const char* p = tile < TK ? kc + blk + tile * 1024 : vc + blk + (tile - TK) * 1024;
+      sr[j] = *(const u32x4*)(p + src);
+    }
+  };
+  auto store_stage = [&](int buf) {
+#pragma unroll
+    for (int j = 0; j < NPW; ++j)
+      *(u32x4*)(lds + buf * (SB * TB * 1024) + (w * NPW + j) * 1024 + lane * 16) = sr[j];
+  };
+  load_stage(0);
+  const float scale2 = a.scale * 1.44269504088896340736f;   // log2 e
+  const float* qrow = a.q + ((size_t)m * a.n_heads + head) * HD + h * 8;
+  bf16x8 qh[DS], ql[DS];
+#pragma unroll
+  for (int ds = 0; ds < DS; ++ds) {
+    const float4 x = *(const float4*)(qrow + ds * 16), z = *(const float4*)(qrow + ds * 16 + 4);
+    const float f = qvalid ? scale2 : 0.f;
+    const float v[8] = {x.x * f, x.y * f, x.z * f, x.w * f, z.x * f, z.y * f, z.z * f, z.w * f};
+    u32x4 hi, lo;
+    split8(v, hi, lo);
+    qh[ds] = as_bf16x8(hi);
+    ql[ds] = as_bf16x8(lo);
+  }
+  float mrun = -INFINITY, lrun = 0.f;
+  f32x16 o[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+  const int key = 16 * (c32 >> 4) + 8 * (c32 >> 2 & 1) + 4 * (c32 >> 3 & 1) + (c32 & 3);
+  const int koff = (key >> 4) * 1024 + h * 256 + (key & 15) * 16;
+  const int voff = TK * 1024 + (c32 >> 4) * 1024 + h * 256 + (c32 & 15) * 16;
+
+  auto block = [&](const char* p) {
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int ds = 0; ds < DS; ++ds) {
+      const bf16x8 kf = as_bf16x8(*(const u32x4*)(p + koff + (ds >> 1) * 2048 + (ds & 1) * 512));
+      s = mfma32_bf16(kf, qh[ds], s);
+      s = mfma32_bf16(kf, ql[ds], s);
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    if (__ballot(mx > mrun + 8.f)) {
+      const float mnew = fmaxf(mrun, mx);
+      const float alpha = mnew == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mrun - mnew);
+      mrun = mnew;
+      lrun *= alpha;
+#pragma unroll
+      for (int t = 0; t < DT; ++t) o[t] *= alpha;
+    }
+    const float b = mrun == -INFINITY ? 0.f : mrun;
+    float pv[2][8], ls[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      pv[i >> 3][i & 7] = __builtin_amdgcn_exp2f(s[i] - b);
+      ls[i & 1] += pv[i >> 3][i & 7];
+    }
+    lrun += ls[0] + ls[1];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      u32x4 hi, lo;
+      split8(pv[c], hi, lo);
+      const bf16x8 ph = as_bf16x8(hi), pl = as_bf16x8(lo);
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        const bf16x8 vf = as_bf16x8(*(const u32x4*)(p + voff + t * 2048 + c * 512));
+        o[t] = mfma32_bf16(vf, ph, o[t]);
+        o[t] = mfma32_bf16(vf, pl, o[t]);
+      }
+    }
+  };
+
+  store_stage(0);
+  __syncthreads();
+  const bool live = (y * QT + qt) * 32 < qn;   // a wave without queries loads for the others
+  for (int st = 0; st < stages; ++st) {
+    if (st + 1 < stages) load_stage(st + 1);
+    const char* buf = lds + (st & 1) * (SB * TB * 1024);
+#pragma unroll
+    for (int b = 0; b < SB; b += KS)
+      if (live && st * SB + b + ks < nblk) block(buf + (b + ks) * (TB * 1024));
+    if (st + 1 < stages) store_stage((st + 1) & 1);
+    __syncthreads();
+  }
+
+  {
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(lrun), __float_as_uint(lrun), false, false);
+    lrun = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  }
+  if constexpr (KS > 1) {   // the tile's waves, in order
+    float2(*ml)[32] = (float2(*)[32])(lds + 2 * SB * TB * 1024);
+    f32x4(*so)[DT * 4][64] = (f32x4(*)[DT * 4][64])lds;
+    if (lane < 32) ml[w][lane] = make_float2(mrun, lrun);
+    if (ks) {
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          so[w - QT][t * 4 + j][lane] = f32x4{o[t][4 * j], o[t][4 * j + 1], o[t][4 * j + 2], o[t][4 * j + 3]};
+    }
+    __syncthreads();
+    if (ks) return;
+    float M = mrun;
+#pragma unroll
+    for (int x = 1; x < KS; ++x) M = fmaxf(M, ml[x * QT + qt][c32].x);
+    const float b = M == -INFINITY ? 0.f : M;
+    const float f0 = __builtin_amdgcn_exp2f(mrun - b);
+    float L = lrun * f0;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) o[t] *= f0;
+#pragma unroll
+    for (int x = 1; x < KS; ++x) {
+      const float2 v = ml[x * QT + qt][c32];
+      const float f = __builtin_amdgcn_exp2f(v.x - b);
+      L += v.y * f;
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4 z = so[x * QT + qt - QT][t * 4 + j][lane];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[t][4 * j + i] += z[i] * f;
+        }
+    }
+    mrun = M;
+    lrun = L;
+  }
+  if (!qvalid) return;
+  const size_t r = ((size_t)slot * a.B * a.R + m) * a.n_heads + head;
+  float* po = a.part_o + r * HD + 4 * h;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *(f32x4*)(po + t * 32 + j * 8) = f32x4{o[t][4 * j], o[t][4 * j + 1], o[t][4 * j + 2], o[t][4 * j + 3]};
+  if (lane < 32) a.part_ml[r] = make_float2(mrun, lrun);
+}
+
+// QT: query tiles of 32 per workgroup of the prefix's parts (tile_part), or 0:
+// 16 queries on the direct path (fp32 caches)
+template <int KVB, int HD, int QT>
 __global__ __launch_bounds__(SW * 64) void k_share(ShareArgs a) {
-  __shared__ __align__(16) char lds[2 * SW * 16 * 4 + SW * HD * 64];
+  constexpr int kDirectLds = 2 * SW * 16 * 4 + SW * HD * 64;
+  constexpr int kTileLds = QT ? tile_lds<HD, QT ? QT : 8>() : 0;
+  __shared__ __align__(16) char lds[kDirectLds > kTileLds ? kDirectLds : kTileLds];
   // ids of one KV head are equal mod n_kv: with eight or a multiple of eight
   // KV heads, the parts that read the same keys run on one XCD
   const int n_prefix = a.n_groups * a.n_kv * a.p_tiles * a.p_chunks;
@@ -328,8 +528,9 @@ __global__ __launch_bounds__(SW * 64) void k_share(ShareArgs a) {
     const int y = id % a.p_tiles, c = id / a.p_tiles;
     const int s = group_prefix(a, g), per = prefix_chunk(s, a.p_chunks);
     const QuerySet qs{g.first * a.R, g.count * a.R, kvh};
-    if (c * per >= s || y * 16 >= qs.rows * (a.n_heads / a.n_kv)) return;
-    direct_part<KVB, HD>(a, qs, KeyRange{g.root, c * per, min(s, c * per + per), INT_MAX}, y, c, lds);
+    if (c * per >= s || y * (QT ? 32 * QT : 16) >= qs.rows * (a.n_heads / a.n_kv)) return;
+    if constexpr (QT > 0) tile_part<HD, QT>(a, qs, g.root, c * per, min(s, c * per + per), y, c, lds);
+    else direct_part<KVB, HD>(a, qs, KeyRange{g.root, c * per, min(s, c * per + per), INT_MAX}, y, c, lds);
     return;
   }
   id -= n_prefix;
@@ -397,33 +598,46 @@ __global__ __launch_bounds__(256) void k_share_join(ShareArgs a) {
   else pack_store4(a.out, a.wtype, m, head * HD + d, y4);
 }
 
-template <int KVB, int HD>
-hipError_t launch_shared_hd(const ShareArgs& a, hipStream_t s) {
+template <int KVB, int HD, int QT>
+hipError_t launch_shared_qt(const ShareArgs& a, hipStream_t s) {
   const long long wgs = (long long)a.n_groups * a.n_kv * a.p_tiles * a.p_chunks + (long long)a.B * a.n_kv * a.t_tiles * a.t_chunks;
   if (wgs > INT_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((k_share<KVB, HD>), dim3((unsigned)wgs), dim3(SW * 64), 0, s, a);
+  hipLaunchKernelGGL((k_share<KVB, HD, QT>), dim3((unsigned)wgs), dim3(SW * 64), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((k_share_join<HD>), dim3(a.B * a.R, (a.n_heads * HD / 4 + 255) / 256), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
-// one workgroup per row: its keys and values, rounded to the cache's type, into
-// slot L_b + i
+template <int HD>
+hipError_t launch_shared_hd(int kv_bf16, const ShareArgs& a, hipStream_t s) {
+  if (!kv_bf16) return launch_shared_qt<0, HD, 0>(a, s);
+  switch (a.p_tile) {
+    case 256: return launch_shared_qt<1, HD, 8>(a, s);
+    case 128: return launch_shared_qt<1, HD, 4>(a, s);
+    case 64: return launch_shared_qt<1, HD, 2>(a, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+// one workgroup per (row, KV head), a thread per dim: the row's keys and values,
+// rounded to the cache's type, into slot L_b + i
 template <typename T>
-__global__ __launch_bounds__(256) void k_kv_append(AppendArgs a) {
-  const int m = blockIdx.x, win = a.window0 + m / a.R;
+__global__ __launch_bounds__(128) void k_kv_append(AppendArgs a) {
+  const int m = blockIdx.x, h = blockIdx.y, win = a.window0 + m / a.R, d = threadIdx.x;
+  const size_t i = ((size_t)m * a.n_kv + h) * a.hd + d;
+  const bool live = d < a.hd;
+  const float k = live ? a.k[i] : 0.f, v = live ? a.v[i] : 0.f;
   const int p = a.lens[win] + m % a.R;
-  if (p >= a.maxlen) return;
-  const int n = a.n_kv * a.hd;
-  auto put = [](T* dst, float x) {
-    if constexpr (sizeof(T) == 2) *dst = f2bf_bits(x);
-    else *dst = x;
-  };
-  for (int i = threadIdx.x; i < n; i += 256) {
-    const size_t base = ((size_t)win * a.n_kv + i / a.hd) * (size_t)a.maxlen * a.hd;
-    put((T*)a.kc + base + kc_off(p, i % a.hd, a.hd), a.k[(size_t)m * n + i]);
-    put((T*)a.vc + base + vc_off(p, i % a.hd, a.hd), a.v[(size_t)m * n + i]);
+  if (!live || p >= a.maxlen) return;
+  const size_t base = ((size_t)win * a.n_kv + h) * (size_t)a.maxlen * a.hd;
+  T *kd = (T*)a.kc + base + kc_off(p, d, a.hd), *vd = (T*)a.vc + base + vc_off(p, d, a.hd);
+  if constexpr (sizeof(T) == 2) {
+    *kd = f2bf_bits(k);
+    *vd = f2bf_bits(v);
+  } else {
+    *kd = k;
+    *vd = v;
   }
 }
 
@@ -504,23 +718,25 @@ __global__ __launch_bounds__(256) void k_kv_fork(ForkArgs a) {
 
 }  // namespace
 
+int share_tile(int kv_bf16, int queries) { return !kv_bf16 ? 16 : queries > 128 ? 256 : queries > 64 ? 128 : 64; }
+
 hipError_t launch_attention_shared(int kv_bf16, int hd, const ShareArgs& a, hipStream_t s) {
   if (a.B < 1 || a.R < 1 || a.t_tiles < 1 || a.t_chunks < 1 || a.n_groups < 0 || a.n_groups > kMaxForkGroups ||
       (a.n_groups && (a.p_tiles < 1 || a.p_chunks < 1)) || a.p_chunks < 0)
     return hipErrorInvalidValue;
   switch (hd) {
-    case 32: return kv_bf16 ? launch_shared_hd<1, 32>(a, s) : launch_shared_hd<0, 32>(a, s);
-    case 64: return kv_bf16 ? launch_shared_hd<1, 64>(a, s) : launch_shared_hd<0, 64>(a, s);
-    case 96: return kv_bf16 ? launch_shared_hd<1, 96>(a, s) : launch_shared_hd<0, 96>(a, s);
-    case 128: return kv_bf16 ? launch_shared_hd<1, 128>(a, s) : launch_shared_hd<0, 128>(a, s);
+    case 32: return launch_shared_hd<32>(kv_bf16, a, s);
+    case 64: return launch_shared_hd<64>(kv_bf16, a, s);
+    case 96: return launch_shared_hd<96>(kv_bf16, a, s);
+    case 128: return launch_shared_hd<128>(kv_bf16, a, s);
   }
   return hipErrorInvalidValue;
 }
 
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t s) {
-  if (a.B < 1 || a.R < 1) return hipErrorInvalidValue;
-  if (a.kv_bf16) hipLaunchKernelGGL((k_kv_append<uint16_t>), dim3(a.B * a.R), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_kv_append<float>), dim3(a.B * a.R), dim3(256), 0, s, a);
+  if (a.B < 1 || a.R < 1 || a.hd > 128) return hipErrorInvalidValue;
+  if (a.kv_bf16) hipLaunchKernelGGL((k_kv_append<uint16_t>), dim3(a.B * a.R, a.n_kv), dim3(128), 0, s, a);
+  else hipLaunchKernelGGL((k_kv_append<float>), dim3(a.B * a.R, a.n_kv), dim3(128), 0, s, a);
   return hipGetLastError();
 }
 
