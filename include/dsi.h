@@ -312,8 +312,8 @@ dsi_status dsi_kv_fork(dsi_kv* kv, int32_t src, int32_t window0, int32_t n_windo
  * q and k come rotated.  rows = 1 is a decoding step.
  *   layer          the layer whose keys and values these are
  *   d_q            [n_windows*rows][n_heads][head_dim] fp32, 16-byte aligned
- *   d_k, d_v       [n_windows*rows][n_kv_heads][head_dim] fp32, rounded to
- *                  kvdtype (nearest even) and stored at slots L_b ..
+ *   d_k, d_v       [n_windows*rows][n_kv_heads][head_dim] fp32, 16-byte aligned,
+ *                  rounded to kvdtype (nearest even) and stored at slots L_b ..
  *   commit         if nonzero, the windows' lengths become L_b + rows (with the
  *                  last layer of a step; a later call overwrites rows that were
  *                  not committed)

@@ -437,8 +437,12 @@ struct ShareGroup {
 };
 struct ShareArgs {
   const float* q;       // [B * R][n_heads * hd]
-  const void* kc;       // layer base
-  const void* vc;
+  void* kc;             // layer base
+  void* vc;
+  // nullable: the rows' keys and values [B * R][n_kv * hd], which are not in the
+  // cache yet: the launch puts them there
+  const float* k_new;
+  const float* v_new;
   ForkState f;
   int window0, B, R;
   int n_heads, n_kv, maxlen;
@@ -448,7 +452,7 @@ struct ShareArgs {
   ShareGroup group[kMaxForkGroups];
   int p_tile;           // queries (rows x heads of one KV head) per workgroup of a prefix: share_tile
   int p_tiles, p_chunks;   // of a group's prefix: query tiles and key chunks at most
-  int t_tiles, t_chunks;   // of a window's own keys: tiles of 16 queries
+  int t_tiles, t_chunks;   // of a window's own keys: tiles of 16 queries; chunks of what the first launch takes of them
   float* part_o;        // [p_chunks + t_chunks][B * R * n_heads][hd]
   float2* part_ml;      // [p_chunks + t_chunks][B * R * n_heads]
   PackRef out;          // O-projection input pack, or
@@ -457,17 +461,6 @@ struct ShareArgs {
 };
 int share_tile(int kv_bf16, int queries);
 hipError_t launch_attention_shared(int kv_bf16, int hd, const ShareArgs& a, hipStream_t s);
-// rows' keys and values [B * R][n_kv * hd] into the cache behind each window's length
-struct AppendArgs {
-  const float* k;
-  const float* v;
-  void* kc;             // layer base
-  void* vc;
-  int kv_bf16;
-  const int* lens;
-  int window0, B, R, n_kv, hd, maxlen;
-};
-hipError_t launch_kv_append(const AppendArgs& a, hipStream_t s);
 hipError_t launch_kv_advance(int* lens, int window0, int B, int rows, hipStream_t s);
 
 // KV and misc (elementwise.hip)

@@ -676,7 +676,7 @@ SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, 
   a.t_chunks = std::min(std::max(1, 512 / (B * m->hkv * a.t_tiles)), cdiv(kv->max_len, 256));
   if (a.n_groups) {
     a.p_tiles = cdiv(G * R * most, a.p_tile);
-    a.p_chunks = std::min(std::max(1, 256 / (a.n_groups * m->hkv * a.p_tiles)), cdiv(kv->max_len, 256));
+    a.p_chunks = std::min(std::max(1, 256 / (a.n_groups * m->hkv * a.p_tiles)), cdiv(kv->max_len, 128));
   }
   p.parts = (size_t)(a.p_chunks + a.t_chunks) * B * R * m->hq;
   return p;
@@ -1930,7 +1930,8 @@ dsi_status dsi_attend(dsi_model* m, dsi_kv* kv, const dsi_attend_args* a) {
     return fail(DSI_EINVAL, "windows [%d, %lld) outside the cache's %d", a->window0, (long long)a->window0 + B,
                 kv->n_windows);
   if (!a->d_q || !a->d_k || !a->d_v || !a->d_out) return fail(DSI_EINVAL, "null queries, keys, values or output pointer");
-  if (((uintptr_t)a->d_q | (uintptr_t)a->d_out) & 15) return fail(DSI_EINVAL, "queries or output not 16-byte aligned");
+  if (((uintptr_t)a->d_q | (uintptr_t)a->d_k | (uintptr_t)a->d_v | (uintptr_t)a->d_out) & 15)
+    return fail(DSI_EINVAL, "queries, keys, values or output not 16-byte aligned");
   (void)capturing(m);
   for (int b = 0; b < B; ++b)
     if (kv->hi[a->window0 + b] + R > kv->max_len)
@@ -1940,21 +1941,9 @@ dsi_status dsi_attend(dsi_model* m, dsi_kv* kv, const dsi_attend_args* a) {
   DSI_TRY(ensure_attention(m, sp.parts));
   ShareArgs sa = share_args(m, kv, sp, a->layer, a->d_q);
   sa.out_rows = a->d_out;
-  AppendArgs pa{};
-  pa.k = a->d_k;
-  pa.v = a->d_v;
-  pa.kc = kv_ptr(kv, kv->k, a->layer, 0);
-  pa.vc = kv_ptr(kv, kv->v, a->layer, 0);
-  pa.kv_bf16 = m->kvb;
-  pa.lens = kv->lens;
-  pa.window0 = a->window0;
-  pa.B = B;
-  pa.R = R;
-  pa.n_kv = m->hkv;
-  pa.hd = m->hd;
-  pa.maxlen = kv->maxlen_pad;
+  sa.k_new = a->d_k;
+  sa.v_new = a->d_v;
   Prof p(m, DSI_K_ATTN);
-  HIP_TRY(launch_kv_append(pa, m->stream));
   HIP_TRY(launch_attention_shared(m->kvb, m->hd, sa, m->stream));
   if (a->commit) {
     HIP_TRY(launch_kv_advance(kv->lens, a->window0, B, R, m->stream));

@@ -9,9 +9,14 @@
 //   M = max m_c,  out = sum_c e^(m_c - M) O_c / sum_c e^(m_c - M) l_c.
 // The keys [0, s) are every row's, so the B R rows of a group are one product
 // without a mask, over one copy of the prefix; the rest is each window's own.
-// One launch runs both kinds of part, a second joins them.
+// The first launch runs the prefix in chunks, and what a window has of its own
+// beyond its last kLast cached keys and the rows of the call (mostly nothing).
+// The second attends to those last keys and joins the parts: rows and masks are
+// its business alone, and no third launch reads what it computed.
 #include <limits.h>
 #include <math.h>
+
+#include <type_traits>
 
 #include "scan.h"
 
@@ -21,8 +26,9 @@ namespace {
 
 constexpr int SW = 8;                  // waves per workgroup
 constexpr int kMinShared = 128;        // a shorter shared prefix is read by each window
-constexpr int kMinPrefixChunk = 256;   // keys per workgroup at least
-constexpr int kTailChunk = SW * 32;    // keys of a window's own per workgroup: a multiple of this
+constexpr int kMinPrefixChunk = 128;   // keys per workgroup at least
+constexpr int kLast = SW * 32;         // cached keys that the second launch takes at most, one step a wave
+constexpr int kOwnChunk = SW * 32;     // keys of a window's own per workgroup of the first launch: a multiple of this
 
 __device__ __forceinline__ int wave_min(int v) {
   dpp_steps([&](auto s) { v = min(v, dpp_from<decltype(s)::ctrl, decltype(s)::rows>(v, v)); });
@@ -51,18 +57,22 @@ __device__ __forceinline__ int window_prefix(const ShareArgs& a, int win) {
 __device__ __forceinline__ int prefix_chunk(int s, int most) {
   return max(kMinPrefixChunk, ((s + most - 1) / most + 63) & ~63);
 }
-__device__ __forceinline__ int tail_chunk(int keys, int most) {
-  return ((keys + most - 1) / most + kTailChunk - 1) / kTailChunk * kTailChunk;
+__device__ __forceinline__ int own_chunk(int keys, int most) {
+  return ((keys + most - 1) / most + kOwnChunk - 1) / kOwnChunk * kOwnChunk;
 }
+// keys [s, own_end) of a window of len cached positions are attended by the
+// first launch: whole blocks, all of them cached
+__device__ __forceinline__ int own_end(int s, int len) { return len - s <= kLast ? s : s + (len - s - 1) / kLast * kLast; }
 
 // Queries of one part: `rows` consecutive rows from row0 on, times the G query
 // heads of KV head kvh; query q is row q % rows of head q / rows.
 struct QuerySet {
   int row0, rows, kvh;
 };
-// Keys [k0, k1) of cache window `win`.  Those from `own` on are the rows of
-// the call: key own + j is seen by rows i >= j of the window (tree: by those
-// that have bit j).
+// Keys [k0, k1) of cache window `win`, k0 a multiple of 32, and k1 too unless
+// the range holds the rows of the call (LAST): those are keys own .. k1 - 1, and
+// key own + j is seen by rows i >= j of the window (tree: by those that have bit
+// j).
 struct KeyRange {
   int win, k0, k1, own;
 };
@@ -71,13 +81,19 @@ struct KeyRange {
 // 32-key step, keys and values straight from the cache into fragments (as in
 // the window attention: 16x16 MFMAs, S^T = K Q^T and O^T += V^T P^T, queries
 // and probabilities of a bf16 cache as hi + lo).  The waves' sums are joined in
-// LDS and leave as chunk `slot` of the partials.
-template <int KVB, int HD>
-__device__ void direct_part(const ShareArgs& a, const QuerySet& qs, const KeyRange& ks, int y, int slot, char* lds) {
-  constexpr int DS = HD / 32, DT = HD / 16;
-  float(*sm)[16] = (float(*)[16])lds;
-  float(*sl)[16] = (float(*)[16])(lds + SW * 16 * 4);
-  f32x4(*so)[DT][64] = (f32x4(*)[DT][64])(lds + 2 * SW * 16 * 4);
+// LDS, where they lie as wave_sums.
+// LAST: the second launch's part, with the rows of the call.  Values are summed
+// for VD of the head's dims, from d0 on.
+template <int VD>
+struct WaveSums {
+  float m[SW][16], l[SW][16];
+  f32x4 o[SW][VD / 16][64];
+};
+
+template <int KVB, int HD, int VD, int LAST>
+__device__ __forceinline__ void direct_sums(const ShareArgs& a, const QuerySet& qs, const KeyRange& ks, int y, int d0,
+                                            WaveSums<VD>& sums) {
+  constexpr int DS = HD / 32, DT = VD / 16;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = a.n_heads / a.n_kv, r16 = lane & 15, kgrp = (lane >> 4) * 8;
@@ -86,11 +102,10 @@ __device__ void direct_part(const ShareArgs& a, const QuerySet& qs, const KeyRan
   const bool qvalid = qi < qn;
   const int gh = qvalid ? qi / qs.rows : 0, ri = qvalid ? qi % qs.rows : 0;
   const int m = qs.row0 + ri, head = qs.kvh * G + gh;
-  const int qpos = !qvalid ? -1 : ks.own == INT_MAX ? INT_MAX : ks.own + ri;
-  const unsigned long long anc = a.anc && qvalid && ks.own != INT_MAX ? a.anc[m] : ~0ull;
+  const int qpos = qvalid ? ks.own + ri : -1;
+  const unsigned long long anc = LAST && a.anc && qvalid ? a.anc[m] : ~0ull;
   const size_t base = ((size_t)ks.win * a.n_kv + qs.kvh) * (size_t)a.maxlen * HD;
   const float scale2 = a.scale * 1.44269504088896340736f;   // log2 e
-
   struct KV16 {
     u32x4 k[2][DS], v[DT];
   };
@@ -118,7 +133,7 @@ __device__ void direct_part(const ShareArgs& a, const QuerySet& qs, const KeyRan
   auto load_v = [&](int p0) {
 #pragma unroll
     for (int t = 0; t < DT; ++t) {
-      const size_t i = base + vc_off(p0 + kgrp, t * 16 + r16, HD);
+      const size_t i = base + vc_off(p0 + kgrp, d0 + t * 16 + r16, HD);
       if (KVB) {
         b16.v[t] = *(const u32x4*)((const uint16_t*)a.vc + i);
       } else {
@@ -178,7 +193,7 @@ __device__ void direct_part(const ShareArgs& a, const QuerySet& qs, const KeyRan
     }
     if (pn < ks.k1) load_k(pn);
     // lane: keys p0 + kgrp + e of query r16, base-2 units
-    const bool full = p0 + 32 <= ks.k1 && (ks.own == INT_MAX || p0 + 32 <= ks.own);
+    const bool full = !LAST || p0 + 32 <= ks.own;
     float pv[8];
     unsigned seen = 0xFF;
     float mloc = -INFINITY;
@@ -257,7 +272,7 @@ __device__ void direct_part(const ShareArgs& a, const QuerySet& qs, const KeyRan
             for (int t = 0; t < DT; ++t)
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                const size_t i = base + vc_off(key, t * 16 + (lane >> 4) * 4 + j, HD);
+                const size_t i = base + vc_off(key, d0 + t * 16 + (lane >> 4) * 4 + j, HD);
                 const float v = KVB ? bf_bits2f(((const uint16_t*)a.vc)[i]) : ((const float*)a.vc)[i];
                 if (!(fabsf(v) < INFINITY)) o[t][j] += p * v;
               }
@@ -285,29 +300,45 @@ __device__ void direct_part(const ShareArgs& a, const QuerySet& qs, const KeyRan
 
   lrun = sum_over_16_32(lrun);
   if (lane < 16) {
-    sm[w][lane] = mrun;
-    sl[w][lane] = lrun;
+    sums.m[w][lane] = mrun;
+    sums.l[w][lane] = lrun;
   }
 #pragma unroll
-  for (int t = 0; t < DT; ++t) so[w][t][lane] = o[t];
+  for (int t = 0; t < DT; ++t) sums.o[w][t][lane] = o[t];
   __syncthreads();
-  const size_t row = (size_t)slot * a.B * a.R * a.n_heads;
-  for (int it = threadIdx.x; it < DT * 64; it += SW * 64) {
-    const int t = it >> 6, l = it & 63, q = l & 15, qc = y * 16 + q;
-    if (qc >= qn) continue;
-    float M = sm[0][q];
+}
+
+// sums of query q (of 16) over the waves: dims 16 t + 4 (l / 16) + 0..3 of it, l % 16 = q
+template <int VD>
+__device__ __forceinline__ void join_waves(const WaveSums<VD>& sums, int t, int l, float& M, float& L, f32x4& acc) {
+  const int q = l & 15;
+  M = sums.m[0][q];
 #pragma unroll
-    for (int x = 1; x < SW; ++x) M = fmaxf(M, sm[x][q]);
-    const float b = M == -INFINITY ? 0.f : M;
-    f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-    float L = 0.f;
+  for (int x = 1; x < SW; ++x) M = fmaxf(M, sums.m[x][q]);
+  const float b = M == -INFINITY ? 0.f : M;
+  acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  L = 0.f;
 #pragma unroll
-    for (int x = 0; x < SW; ++x) {
-      const float f = __builtin_amdgcn_exp2f(sm[x][q] - b);
-      acc += so[x][t][l] * f;
-      L += sl[x][q] * f;
-    }
-    const size_t r = row + (size_t)(qs.row0 + qc % qs.rows) * a.n_heads + qs.kvh * G + qc / qs.rows;
+  for (int x = 0; x < SW; ++x) {
+    const float f = __builtin_amdgcn_exp2f(sums.m[x][q] - b);
+    acc += sums.o[x][t][l] * f;
+    L += sums.l[x][q] * f;
+  }
+}
+
+// 16 queries over keys without a mask, as chunk `slot` of the partials
+template <int KVB, int HD>
+__device__ void direct_part(const ShareArgs& a, const QuerySet& qs, int win, int k0, int k1, int y, int slot, char* lds) {
+  WaveSums<HD>& sums = *(WaveSums<HD>*)lds;
+  direct_sums<KVB, HD, HD, 0>(a, qs, KeyRange{win, k0, k1, 0}, y, 0, sums);
+  const int G = a.n_heads / a.n_kv;
+  for (int it = threadIdx.x; it < HD / 16 * 64; it += SW * 64) {
+    const int t = it >> 6, l = it & 63, qc = y * 16 + (l & 15);
+    if (qc >= G * qs.rows) continue;
+    float M, L;
+    f32x4 acc;
+    join_waves(sums, t, l, M, L, acc);
+    const size_t r = ((size_t)slot * a.B * a.R + qs.row0 + qc % qs.rows) * a.n_heads + qs.kvh * G + qc / qs.rows;
     *(f32x4*)(a.part_o + r * HD + t * 16 + (l >> 4) * 4) = acc;
     if (t == 0 && l < 16) a.part_ml[r] = make_float2(M, L);
   }
@@ -330,9 +361,10 @@ __device__ __forceinline__ f32x16 mfma32_bf16(const bf16x8& a, const bf16x8& b, 
 // the 16 scores a lane gets are keys 16 c + 8 (l / 32) + 0..7, c = 0, 1: its
 // B operands of the second product.
 // A block of the cache is HD / 16 tiles of 1 KB for K (16 positions x 32 dims)
-// and for V (16 dims x 32 positions); 16-byte piece (row r, piece 2 c + h) of a
-// tile sits at c * 512 + h * 256 + r * 16 in LDS, so that every 16 lanes of a
-// fragment read 256 consecutive bytes.
+// and for V (16 dims x 32 positions), rows of four 16-byte pieces.  They are
+// loaded as they lie; piece q of row r goes to r * 64 + (q ^ r / 4 % 4) * 16 in
+// LDS, so that the 16 rows a fragment read takes the same piece of lie in 16
+// different groups of banks.
 // Queries (times scale and log2 e) and probabilities are hi + lo bf16, as in
 // the window attention; the running maximum moves only when a score is 2^8 above
 // it, so most blocks rescale nothing.
@@ -357,7 +389,7 @@ __device__ void tile_part(const ShareArgs& a, const QuerySet& qs, int win, int k
   const char* kc = (const char*)a.kc + base;
   const char* vc = (const char*)a.vc + base;
   const int blk0 = k0 >> 5, nblk = (k1 - k0) >> 5, stages = (nblk + SB - 1) / SB;
-  const int src = (lane & 15) * 64 + (lane >> 4) * 16;   // of this lane's piece in a tile
+  const int dst = (lane >> 2) * 64 + ((lane & 3) ^ (lane >> 4)) * 16;   // of this lane's piece in a tile in LDS
 
   u32x4 sr[NPW];
   auto load_stage = [&](int st) {
@@ -366,13 +398,13 @@ __device__ void tile_part(const ShareArgs& a, const QuerySet& qs, int win, int k
       const int i = w * NPW + j, tile = i % TB;
       const size_t blk = (size_t)(blk0 + min(st * SB + i / TB, nblk - 1)) * (HD * 64);
       const char* p = tile < TK ? kc + blk + tile * 1024 : vc + blk + (tile - TK) * 1024;
-      sr[j] = *(const u32x4*)(p + src);
+      sr[j] = *(const u32x4*)(p + lane * 16);
     }
   };
   auto store_stage = [&](int buf) {
 #pragma unroll
     for (int j = 0; j < NPW; ++j)
-      *(u32x4*)(lds + buf * (SB * TB * 1024) + (w * NPW + j) * 1024 + lane * 16) = sr[j];
+      *(u32x4*)(lds + buf * (SB * TB * 1024) + (w * NPW + j) * 1024 + dst) = sr[j];
   };
   load_stage(0);
   const float scale2 = a.scale * 1.44269504088896340736f;   // log2 e
@@ -395,22 +427,36 @@ __device__ void tile_part(const ShareArgs& a, const QuerySet& qs, int win, int k
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
   const int key = 16 * (c32 >> 4) + 8 * (c32 >> 2 & 1) + 4 * (c32 >> 3 & 1) + (c32 & 3);
-  const int koff = (key >> 4) * 1024 + h * 256 + (key & 15) * 16;
-  const int voff = TK * 1024 + (c32 >> 4) * 1024 + h * 256 + (c32 & 15) * 16;
+  const int koff = (key >> 4) * 1024 + (key & 15) * 64 + (h ^ (key >> 2 & 3)) * 16;
+  const int voff = TK * 1024 + (c32 >> 4) * 1024 + (c32 & 15) * 64 + (h ^ (c32 >> 2 & 3)) * 16;
 
-  auto block = [&](const char* p) {
-    f32x16 s;
+  // NB blocks of 32 keys at once, at p and TB KB apart: two independent chains
+  // of matrix instructions either way
+  constexpr int NB = 1;
+  auto blocks = [&](const char* p, auto full) {
+    constexpr int N = decltype(full)::value;
+    f32x16 s[2];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
 #pragma unroll
     for (int ds = 0; ds < DS; ++ds) {
-      const bf16x8 kf = as_bf16x8(*(const u32x4*)(p + koff + (ds >> 1) * 2048 + (ds & 1) * 512));
-      s = mfma32_bf16(kf, qh[ds], s);
-      s = mfma32_bf16(kf, ql[ds], s);
+      const int at = (koff ^ (ds & 1) * 32) + (ds >> 1) * 2048;
+      const bf16x8 k0 = as_bf16x8(*(const u32x4*)(p + at));
+      if constexpr (N == 2) {
+        const bf16x8 k1 = as_bf16x8(*(const u32x4*)(p + TB * 1024 + at));
+        s[0] = mfma32_bf16(k0, qh[ds], s[0]);
+        s[1] = mfma32_bf16(k1, qh[ds], s[1]);
+        s[0] = mfma32_bf16(k0, ql[ds], s[0]);
+        s[1] = mfma32_bf16(k1, ql[ds], s[1]);
+      } else {
+        s[0] = mfma32_bf16(k0, qh[ds], s[0]);
+        s[1] = mfma32_bf16(k0, ql[ds], s[1]);
+      }
     }
-    float mx = s[0];
+    if constexpr (N == 1) s[0] += s[1];
+    float mx = s[0][0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    for (int i = 1; i < 16 * N; ++i) mx = fmaxf(mx, s[i >> 4][i & 15]);
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
     mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
     if (__ballot(mx > mrun + 8.f)) {
@@ -422,36 +468,42 @@ __device__ void tile_part(const ShareArgs& a, const QuerySet& qs, int win, int k
       for (int t = 0; t < DT; ++t) o[t] *= alpha;
     }
     const float b = mrun == -INFINITY ? 0.f : mrun;
-    float pv[2][8], ls[2] = {0.f, 0.f};
+    float ls[2] = {0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      pv[i >> 3][i & 7] = __builtin_amdgcn_exp2f(s[i] - b);
-      ls[i & 1] += pv[i >> 3][i & 7];
+    for (int c = 0; c < 2 * N; ++c) {   // 16 keys
+      float pv[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        pv[i] = __builtin_amdgcn_exp2f(s[c >> 1][(c & 1) * 8 + i] - b);
+        ls[i & 1] += pv[i];
+      }
+      u32x4 hi, lo;
+      split8(pv, hi, lo);
+      const bf16x8 ph = as_bf16x8(hi), pl = as_bf16x8(lo);
+      bf16x8 vf[DT];
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+        vf[t] = as_bf16x8(*(const u32x4*)(p + (c >> 1) * (TB * 1024) + (voff ^ (c & 1) * 32) + t * 2048));
+#pragma unroll
+      for (int t = 0; t < DT; ++t) o[t] = mfma32_bf16(vf[t], ph, o[t]);
+#pragma unroll
+      for (int t = 0; t < DT; ++t) o[t] = mfma32_bf16(vf[t], pl, o[t]);
     }
     lrun += ls[0] + ls[1];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      u32x4 hi, lo;
-      split8(pv[c], hi, lo);
-      const bf16x8 ph = as_bf16x8(hi), pl = as_bf16x8(lo);
-#pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        const bf16x8 vf = as_bf16x8(*(const u32x4*)(p + voff + t * 2048 + c * 512));
-        o[t] = mfma32_bf16(vf, ph, o[t]);
-        o[t] = mfma32_bf16(vf, pl, o[t]);
-      }
-    }
   };
 
+  const bool live = (y * QT + qt) * 32 < qn;   // a wave without queries loads for the others
+  auto compute = [&](int st) {
+    const char* p = lds + (st & 1) * (SB * TB * 1024);
+#pragma unroll
+    for (int i = 0; i < SB; i += KS)
+      if (live && st * SB + i + ks < nblk) blocks(p + (i + ks) * (TB * 1024), std::integral_constant<int, 1>{});
+  };
   store_stage(0);
   __syncthreads();
-  const bool live = (y * QT + qt) * 32 < qn;   // a wave without queries loads for the others
   for (int st = 0; st < stages; ++st) {
     if (st + 1 < stages) load_stage(st + 1);
-    const char* buf = lds + (st & 1) * (SB * TB * 1024);
-#pragma unroll
-    for (int b = 0; b < SB; b += KS)
-      if (live && st * SB + b + ks < nblk) block(buf + (b + ks) * (TB * 1024));
+    compute(st);
     if (st + 1 < stages) store_stage((st + 1) & 1);
     __syncthreads();
   }
@@ -509,11 +561,34 @@ __device__ void tile_part(const ShareArgs& a, const QuerySet& qs, int win, int k
   if (lane < 32) a.part_ml[r] = make_float2(mrun, lrun);
 }
 
-// QT: query tiles of 32 per workgroup of the prefix's parts (tile_part), or 0:
-// 16 queries on the direct path (fp32 caches)
+// the rows' keys and values of one window and KV head into the slots behind its
+// length, rounded to the cache's type: keys by dims, values by positions, so that
+// neighbouring threads write neighbours
+template <int KVB, int HD>
+__device__ void append_rows(const ShareArgs& a, int win, int kvh) {
+  const int len = a.f.lens[a.window0 + win];
+  const int n = min(a.R, a.maxlen - len);
+  const size_t base = ((size_t)(a.window0 + win) * a.n_kv + kvh) * (size_t)a.maxlen * HD;
+  const size_t row = (size_t)a.n_kv * HD, from = (size_t)win * a.R * row + (size_t)kvh * HD;
+  for (int i = threadIdx.x; i < n * HD; i += SW * 64) {
+    const int kj = i / HD, kd = i % HD, vj = i % n, vd = i / n;
+    const float k = a.k_new[from + kj * row + kd], v = a.v_new[from + vj * row + vd];
+    const size_t ki = base + kc_off(len + kj, kd, HD), vi = base + vc_off(len + vj, vd, HD);
+    if (KVB) {
+      ((uint16_t*)a.kc)[ki] = f2bf_bits(k);
+      ((uint16_t*)a.vc)[vi] = f2bf_bits(v);
+    } else {
+      ((float*)a.kc)[ki] = k;
+      ((float*)a.vc)[vi] = v;
+    }
+  }
+}
+
+// First launch.  QT: query tiles of 32 per workgroup of the prefix's parts
+// (tile_part), or 0: 16 queries on the direct path (fp32 caches)
 template <int KVB, int HD, int QT>
 __global__ __launch_bounds__(SW * 64) void k_share(ShareArgs a) {
-  constexpr int kDirectLds = 2 * SW * 16 * 4 + SW * HD * 64;
+  constexpr int kDirectLds = sizeof(WaveSums<HD>);
   constexpr int kTileLds = QT ? tile_lds<HD, QT ? QT : 8>() : 0;
   __shared__ __align__(16) char lds[kDirectLds > kTileLds ? kDirectLds : kTileLds];
   // ids of one KV head are equal mod n_kv: with eight or a multiple of eight
@@ -530,7 +605,7 @@ __global__ __launch_bounds__(SW * 64) void k_share(ShareArgs a) {
     const QuerySet qs{g.first * a.R, g.count * a.R, kvh};
     if (c * per >= s || y * (QT ? 32 * QT : 16) >= qs.rows * (a.n_heads / a.n_kv)) return;
     if constexpr (QT > 0) tile_part<HD, QT>(a, qs, g.root, c * per, min(s, c * per + per), y, c, lds);
-    else direct_part<KVB, HD>(a, qs, KeyRange{g.root, c * per, min(s, c * per + per), INT_MAX}, y, c, lds);
+    else direct_part<KVB, HD>(a, qs, g.root, c * per, min(s, c * per + per), y, c, lds);
     return;
   }
   id -= n_prefix;
@@ -539,73 +614,88 @@ __global__ __launch_bounds__(SW * 64) void k_share(ShareArgs a) {
   const int win = id % a.B;
   id /= a.B;
   const int y = id % a.t_tiles, c = id / a.t_tiles;
+  // no part of this launch reads the slots of the call's rows
+  if (a.k_new && y == 0 && c == 0) append_rows<KVB, HD>(a, win, kvh);
   const int s = window_prefix(a, win);
-  const int len = min(a.f.lens[a.window0 + win], a.maxlen - a.R);
-  const int keys = len + a.R - s, per = tail_chunk(keys, a.t_chunks);
+  const int keys = own_end(s, min(a.f.lens[a.window0 + win], a.maxlen - a.R)) - s, per = own_chunk(keys, a.t_chunks);
   if (c * per >= keys) return;
-  direct_part<KVB, HD>(a, QuerySet{win * a.R, a.R, kvh},
-                       KeyRange{a.window0 + win, s + c * per, min(len + a.R, s + c * per + per), len}, y, a.p_chunks + c,
-                       lds);
+  direct_part<KVB, HD>(a, QuerySet{win * a.R, a.R, kvh}, a.window0 + win, s + c * per, s + min(keys, c * per + per), y,
+                       a.p_chunks + c, lds);
 }
 
-// Joins the parts of every (row, head), in order: one workgroup per row and 256
-// pieces of four dims.
-template <int HD>
-__global__ __launch_bounds__(256) void k_share_join(ShareArgs a) {
-  const int m = blockIdx.x, win = m / a.R;
-  const int i = blockIdx.y * 256 + threadIdx.x;
+// Second launch: one workgroup per (window, KV head, 16 queries, VD dims) attends
+// to the window's last keys and the rows, and joins that with the partials of its
+// queries, in order.  Heads of more than 64 dims are halved: twice the workgroups
+// read the partials, for a second reading of the few keys.
+template <int KVB, int HD>
+__global__ __launch_bounds__(SW * 64) void k_share_last(ShareArgs a) {
+  constexpr int NV = HD > 64 ? 2 : 1, VD = HD / NV, CB = 8;
+  __shared__ __align__(16) WaveSums<VD> sums;
+  int id = blockIdx.x;
+  const int kvh = id % a.n_kv;
+  id /= a.n_kv;
+  const int d0 = id % NV * VD;
+  id /= NV;
+  const int win = id % a.B, y = id / a.B;
   const int s = window_prefix(a, win);
-  const int keys = min(a.f.lens[a.window0 + win], a.maxlen - a.R) + a.R - s;
+  const int len = min(a.f.lens[a.window0 + win], a.maxlen - a.R);
+  const int e = own_end(s, len);
   const int np = s ? (s + prefix_chunk(s, a.p_chunks) - 1) / prefix_chunk(s, a.p_chunks) : 0;
-  const int nt = (keys + tail_chunk(keys, a.t_chunks) - 1) / tail_chunk(keys, a.t_chunks);
-  if (i >= a.n_heads * HD / 4) return;
-  const int head = i / (HD / 4), d = i % (HD / 4) * 4;
-  const size_t rows = (size_t)a.B * a.R * a.n_heads, r = (size_t)m * a.n_heads + head;
-  constexpr int CB = 8;
-  float M = -INFINITY, base = 0.f, L = 0.f;
-  f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int c0 = 0; c0 < np + nt; c0 += CB) {
-    float2 ml[CB];
-    f32x4 o[CB];
+  const int nc = np + (e > s ? (e - s + own_chunk(e - s, a.t_chunks) - 1) / own_chunk(e - s, a.t_chunks) : 0);
+  const int G = a.n_heads / a.n_kv;
+  const size_t rows = (size_t)a.B * a.R * a.n_heads;
+  direct_sums<KVB, HD, VD, 1>(a, QuerySet{win * a.R, a.R, kvh}, KeyRange{a.window0 + win, e, len + a.R, len}, y, d0, sums);
+  // the 64 pieces of four dims of each 16 dims on one wave
+  for (int it = threadIdx.x; it < VD / 16 * 64; it += SW * 64) {
+    const int t = it >> 6, l = it & 63, qc = y * 16 + (l & 15);
+    if (qc >= G * a.R) continue;
+    const int m = win * a.R + qc % a.R, head = kvh * G + qc / a.R, d = d0 + t * 16 + (l >> 4) * 4;
+    const size_t r = (size_t)m * a.n_heads + head;
+    float M, L;
+    f32x4 acc;
+    join_waves(sums, t, l, M, L, acc);
+    for (int c0 = 0; c0 < nc; c0 += CB) {
+      float2 ml[CB];
+      f32x4 o[CB];
 #pragma unroll
-    for (int j = 0; j < CB; ++j)
-      if (c0 + j < np + nt) {
-        const size_t slot = (size_t)(c0 + j < np ? c0 + j : a.p_chunks + c0 + j - np) * rows + r;
+      for (int j = 0; j < CB; ++j) {
+        const int c = min(c0 + j, nc - 1);
+        const size_t slot = (size_t)(c < np ? c : a.p_chunks + c - np) * rows + r;
         ml[j] = a.part_ml[slot];
         o[j] = *(const f32x4*)(a.part_o + slot * HD + d);
       }
+      float Mn = M;
 #pragma unroll
-    for (int j = 0; j < CB; ++j)
-      if (c0 + j < np + nt) M = fmaxf(M, ml[j].x);
-    const float b = M == -INFINITY ? 0.f : M;
-    if (c0) {
-      const float f = __builtin_amdgcn_exp2f(base - b);
-      L *= f;
-      acc *= f;
+      for (int j = 0; j < CB; ++j) Mn = fmaxf(Mn, ml[j].x);
+      const float b = Mn == -INFINITY ? 0.f : Mn;
+      const float f0 = __builtin_amdgcn_exp2f(M - b);
+      L *= f0;
+      acc *= f0;
+      M = Mn;
+#pragma unroll
+      for (int j = 0; j < CB; ++j)
+        if (c0 + j < nc) {
+          const float f = __builtin_amdgcn_exp2f(ml[j].x - b);
+          L += ml[j].y * f;
+          acc += o[j] * f;
+        }
     }
-    base = b;
-#pragma unroll
-    for (int j = 0; j < CB; ++j)
-      if (c0 + j < np + nt) {
-        const float f = __builtin_amdgcn_exp2f(ml[j].x - b);
-        L += ml[j].y * f;
-        acc += o[j] * f;
-      }
+    const float inv = 1.0f / L;
+    const float y4[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+    if (a.out_rows) *(float4*)(a.out_rows + r * HD + d) = float4{y4[0], y4[1], y4[2], y4[3]};
+    else pack_store4(a.out, a.wtype, m, head * HD + d, y4);
   }
-  const float inv = 1.0f / L;
-  const float y4[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
-  if (a.out_rows) *(float4*)(a.out_rows + r * HD + d) = float4{y4[0], y4[1], y4[2], y4[3]};
-  else pack_store4(a.out, a.wtype, m, head * HD + d, y4);
 }
 
 template <int KVB, int HD, int QT>
 hipError_t launch_shared_qt(const ShareArgs& a, hipStream_t s) {
   const long long wgs = (long long)a.n_groups * a.n_kv * a.p_tiles * a.p_chunks + (long long)a.B * a.n_kv * a.t_tiles * a.t_chunks;
   if (wgs > INT_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((k_share<KVB, HD, QT>), dim3((unsigned)wgs), dim3(SW * 64), 0, s, a);
+  if (wgs) hipLaunchKernelGGL((k_share<KVB, HD, QT>), dim3((unsigned)wgs), dim3(SW * 64), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_share_join<HD>), dim3(a.B * a.R, (a.n_heads * HD / 4 + 255) / 256), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((k_share_last<KVB, HD>), dim3((unsigned)a.B * a.n_kv * a.t_tiles * (HD > 64 ? 2 : 1)), dim3(SW * 64),
+                     0, s, a);
   return hipGetLastError();
 }
 
@@ -618,27 +708,6 @@ hipError_t launch_shared_hd(int kv_bf16, const ShareArgs& a, hipStream_t s) {
     case 64: return launch_shared_qt<1, HD, 2>(a, s);
   }
   return hipErrorInvalidValue;
-}
-
-// one workgroup per (row, KV head), a thread per dim: the row's keys and values,
-// rounded to the cache's type, into slot L_b + i
-template <typename T>
-__global__ __launch_bounds__(128) void k_kv_append(AppendArgs a) {
-  const int m = blockIdx.x, h = blockIdx.y, win = a.window0 + m / a.R, d = threadIdx.x;
-  const size_t i = ((size_t)m * a.n_kv + h) * a.hd + d;
-  const bool live = d < a.hd;
-  const float k = live ? a.k[i] : 0.f, v = live ? a.v[i] : 0.f;
-  const int p = a.lens[win] + m % a.R;
-  if (!live || p >= a.maxlen) return;
-  const size_t base = ((size_t)win * a.n_kv + h) * (size_t)a.maxlen * a.hd;
-  T *kd = (T*)a.kc + base + kc_off(p, d, a.hd), *vd = (T*)a.vc + base + vc_off(p, d, a.hd);
-  if constexpr (sizeof(T) == 2) {
-    *kd = f2bf_bits(k);
-    *vd = f2bf_bits(v);
-  } else {
-    *kd = k;
-    *vd = v;
-  }
 }
 
 __global__ void k_kv_advance(int* lens, int window0, int B, int rows) {
@@ -721,7 +790,7 @@ __global__ __launch_bounds__(256) void k_kv_fork(ForkArgs a) {
 int share_tile(int kv_bf16, int queries) { return !kv_bf16 ? 16 : queries > 128 ? 256 : queries > 64 ? 128 : 64; }
 
 hipError_t launch_attention_shared(int kv_bf16, int hd, const ShareArgs& a, hipStream_t s) {
-  if (a.B < 1 || a.R < 1 || a.t_tiles < 1 || a.t_chunks < 1 || a.n_groups < 0 || a.n_groups > kMaxForkGroups ||
+  if (a.B < 1 || a.R < 1 || a.t_tiles < 1 || a.t_chunks < 0 || (a.k_new && a.t_chunks < 1) || a.n_groups < 0 || a.n_groups > kMaxForkGroups ||
       (a.n_groups && (a.p_tiles < 1 || a.p_chunks < 1)) || a.p_chunks < 0)
     return hipErrorInvalidValue;
   switch (hd) {
@@ -731,13 +800,6 @@ hipError_t launch_attention_shared(int kv_bf16, int hd, const ShareArgs& a, hipS
     case 128: return launch_shared_hd<128>(kv_bf16, a, s);
   }
   return hipErrorInvalidValue;
-}
-
-hipError_t launch_kv_append(const AppendArgs& a, hipStream_t s) {
-  if (a.B < 1 || a.R < 1 || a.hd > 128) return hipErrorInvalidValue;
-  if (a.kv_bf16) hipLaunchKernelGGL((k_kv_append<uint16_t>), dim3(a.B * a.R, a.n_kv), dim3(128), 0, s, a);
-  else hipLaunchKernelGGL((k_kv_append<float>), dim3(a.B * a.R, a.n_kv), dim3(128), 0, s, a);
-  return hipGetLastError();
 }
 
 hipError_t launch_kv_advance(int* lens, int window0, int B, int rows, hipStream_t s) {

@@ -83,7 +83,7 @@ def test_attend_refusals(stub):
         return 0
     assert status(other) == dsi.DSI_EINVAL
     for change in (dict(layer=-1), dict(layer=3), dict(n_windows=0), dict(rows=0), dict(rows=257), dict(n_windows=5), dict(window0=1),
-                   dict(window0=-1), dict(d_q=None), dict(d_k=None), dict(d_v=None), dict(d_out=None), dict(d_q=P + 4), dict(d_out=P + 8),
+                   dict(window0=-1), dict(d_q=None), dict(d_k=None), dict(d_v=None), dict(d_out=None), dict(d_q=P + 4), dict(d_out=P + 8), dict(d_k=P + 4), dict(d_v=P + 8),
                    dict(window0=2 ** 31 - 1), dict(n_windows=2 ** 31 - 1, rows=2 ** 31 - 1)):
         assert status(**change) == dsi.DSI_EINVAL, change
     assert status(rows=101, n_windows=1) == dsi.DSI_ECAPACITY
@@ -124,7 +124,7 @@ def test_what_runs_and_what_is_allocated(stub):
     dsi.dsi_kv_fork(kv, 4, 5, 1)
     assert "k_share" in verify(4, 2)
     attend = lambda rows, n=8: names(lambda: dsi.dsi_attend(m, kv, 0, 0, n, rows, P, P, P, P))
-    assert attend(20) == {"k_kv_append", "k_share", "k_share_join"}
+    assert attend(20) == {"k_share", "k_share_last"}
     for rows in (20, 1, 7):
         attend(rows)
         assert hip.stub_mallocs() == 0, rows
