@@ -24,10 +24,11 @@ namespace dsi {
 
 namespace {
 
-constexpr int SW = 8;                  // waves per workgroup
+constexpr int SW = 8;                  // waves per workgroup of the first launch
+constexpr int LW = 4;                  // and of the second
 constexpr int kMinShared = 128;        // a shorter shared prefix is read by each window
 constexpr int kMinPrefixChunk = 128;   // keys per workgroup at least
-constexpr int kLast = SW * 32;         // cached keys that the second launch takes at most, one step a wave
+constexpr int kLast = 256;             // cached keys that the second launch takes at most
 constexpr int kOwnChunk = SW * 32;     // keys of a window's own per workgroup of the first launch: a multiple of this
 
 __device__ __forceinline__ int wave_min(int v) {
@@ -84,15 +85,17 @@ struct KeyRange {
 // LDS, where they lie as wave_sums.
 // LAST: the second launch's part, with the rows of the call.  Values are summed
 // for VD of the head's dims, from d0 on.
-template <int VD>
+template <int NW, int VD>
 struct WaveSums {
-  float m[SW][16], l[SW][16];
-  f32x4 o[SW][VD / 16][64];
+  float m[NW][16], l[NW][16];
+  f32x4 o[NW][VD / 16][64];
 };
 
-template <int KVB, int HD, int VD, int LAST>
-__device__ __forceinline__ void direct_sums(const ShareArgs& a, const QuerySet& qs, const KeyRange& ks, int y, int d0,
-                                            WaveSums<VD>& sums) {
+// range(): the keys, which depend on lengths in memory; asked for once the loads
+// of the queries are on their way
+template <int KVB, int HD, int VD, int LAST, int NW, typename F>
+__device__ __forceinline__ void direct_sums(const ShareArgs& a, const QuerySet& qs, F&& range, int y, int d0,
+                                            WaveSums<NW, VD>& sums) {
   constexpr int DS = HD / 32, DT = VD / 16;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -102,8 +105,16 @@ __device__ __forceinline__ void direct_sums(const ShareArgs& a, const QuerySet& 
   const bool qvalid = qi < qn;
   const int gh = qvalid ? qi / qs.rows : 0, ri = qvalid ? qi % qs.rows : 0;
   const int m = qs.row0 + ri, head = qs.kvh * G + gh;
-  const int qpos = qvalid ? ks.own + ri : -1;
   const unsigned long long anc = LAST && a.anc && qvalid ? a.anc[m] : ~0ull;
+  const float* qrow = a.q + (size_t)m * (a.n_heads * HD) + head * HD;
+  F8 qf[DS];
+#pragma unroll
+  for (int ds = 0; ds < DS; ++ds) {   // an invalid lane reads its first row, and drops it
+    qf[ds].a = *(const float4*)(qrow + ds * 32 + kgrp);
+    qf[ds].b = *(const float4*)(qrow + ds * 32 + kgrp + 4);
+  }
+  const KeyRange ks = range();
+  const int qpos = qvalid ? ks.own + ri : -1;
   const size_t base = ((size_t)ks.win * a.n_kv + qs.kvh) * (size_t)a.maxlen * HD;
   const float scale2 = a.scale * 1.44269504088896340736f;   // log2 e
   struct KV16 {
@@ -142,12 +153,17 @@ __device__ __forceinline__ void direct_sums(const ShareArgs& a, const QuerySet& 
       }
     }
   };
-  const float* qrow = a.q + (size_t)m * (a.n_heads * HD) + head * HD;
-  F8 qf[DS];
+  // the first loads of a wave without keys (its step lies past k1) are of the
+  // part's first keys and not used: registers that are loaded on one path only
+  // are not left to the compiler
+  int p0 = ks.k0 + 32 * w;
+  load_k(p0 < ks.k1 ? p0 : ks.k0);
+  load_v(p0 < ks.k1 ? p0 : ks.k0);
 #pragma unroll
   for (int ds = 0; ds < DS; ++ds) {
-    qf[ds].a = qvalid ? *(const float4*)(qrow + ds * 32 + kgrp) : float4{0.f, 0.f, 0.f, 0.f};
-    qf[ds].b = qvalid ? *(const float4*)(qrow + ds * 32 + kgrp + 4) : float4{0.f, 0.f, 0.f, 0.f};
+    const float4 x = qf[ds].a, z = qf[ds].b;
+    qf[ds].a = float4{qvalid ? x.x : 0.f, qvalid ? x.y : 0.f, qvalid ? x.z : 0.f, qvalid ? x.w : 0.f};
+    qf[ds].b = float4{qvalid ? z.x : 0.f, qvalid ? z.y : 0.f, qvalid ? z.z : 0.f, qvalid ? z.w : 0.f};
   }
   bf16x8 qh[DS], ql[DS];
   if (KVB) {
@@ -167,14 +183,8 @@ __device__ __forceinline__ void direct_sums(const ShareArgs& a, const QuerySet& 
 #pragma unroll
   for (int t = 0; t < DT; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // the first loads of a wave without keys (its step lies past k1) are of the
-  // part's first keys and not used: registers that are loaded on one path only
-  // are not left to the compiler
-  int p0 = ks.k0 + 32 * w;
-  load_k(p0 < ks.k1 ? p0 : ks.k0);
-  load_v(p0 < ks.k1 ? p0 : ks.k0);
-  for (; p0 < ks.k1; p0 += 32 * SW) {
-    const int pn = p0 + 32 * SW;
+  for (; p0 < ks.k1; p0 += 32 * NW) {
+    const int pn = p0 + 32 * NW;
     f32x4 st[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -236,47 +246,69 @@ __device__ __forceinline__ void direct_sums(const ShareArgs& a, const QuerySet& 
     if (!full) {
       const int nv = ks.k1 - (p0 + kgrp);
       bool odd = false;
+      if (KVB) {
+        uint32_t keep[4];
 #pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        if (KVB) {
+        for (int i = 0; i < 4; ++i) keep[i] = (2 * i < nv ? 0x0000FFFFu : 0u) | (2 * i + 1 < nv ? 0xFFFF0000u : 0u);
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            uint32_t x = b16.v[t][i] & ((2 * i < nv ? 0x0000FFFFu : 0u) | (2 * i + 1 < nv ? 0xFFFF0000u : 0u));
-            const bool lo = (x & 0x7F80u) == 0x7F80u, hi = (x & 0x7F800000u) == 0x7F800000u;
-            odd |= lo || hi;
-            x &= (lo ? 0u : 0x0000FFFFu) | (hi ? 0u : 0xFFFF0000u);
+            const uint32_t x = b16.v[t][i] & keep[i];
             b16.v[t][i] = x;
+            odd = odd || (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u;
           }
-        } else {
+      } else {
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
           float x[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             x[e] = e < nv ? f8_get(b32.v[t], e) : 0.f;
-            const bool bad = !(fabsf(x[e]) < INFINITY);
-            odd |= bad;
-            x[e] = bad ? 0.f : x[e];
+            odd = odd || !(fabsf(x[e]) < INFINITY);
           }
           b32.v[t].a = float4{x[0], x[1], x[2], x[3]};
           b32.v[t].b = float4{x[4], x[5], x[6], x[7]};
         }
       }
       if (__ballot(odd)) {
-        for (int g = 0; g < 4; ++g)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float p = __shfl(pv[e], r16 + 16 * g);
-            const unsigned vis = __shfl(seen, r16 + 16 * g);
-            const int key = p0 + 8 * g + e;
-            if (!(vis >> e & 1)) continue;
+        for (int t = 0; t < DT; ++t) {
+          if (KVB) {
 #pragma unroll
-            for (int t = 0; t < DT; ++t)
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t x = b16.v[t][i];
+              b16.v[t][i] = x & (((x & 0x7F80u) == 0x7F80u ? 0u : 0x0000FFFFu) | ((x & 0x7F800000u) == 0x7F800000u ? 0u : 0xFFFF0000u));
+            }
+          } else {
+            float x[8];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const size_t i = base + vc_off(key, d0 + t * 16 + (lane >> 4) * 4 + j, HD);
-                const float v = KVB ? bf_bits2f(((const uint16_t*)a.vc)[i]) : ((const float*)a.vc)[i];
-                if (!(fabsf(v) < INFINITY)) o[t][j] += p * v;
-              }
+            for (int e = 0; e < 8; ++e) {
+              x[e] = f8_get(b32.v[t], e);
+              x[e] = fabsf(x[e]) < INFINITY ? x[e] : 0.f;
+            }
+            b32.v[t].a = float4{x[0], x[1], x[2], x[3]};
+            b32.v[t].b = float4{x[4], x[5], x[6], x[7]};
           }
+        }
+        // rolled: the usual step pays no registers for it
+#pragma unroll 1
+        for (int k = 0; k < 32; ++k) {
+          float pe = pv[0];
+#pragma unroll
+          for (int e = 1; e < 8; ++e) pe = (k & 7) == e ? pv[e] : pe;
+          const float p = __shfl(pe, r16 + 16 * (k >> 3));
+          const unsigned vis = __shfl(seen, r16 + 16 * (k >> 3));
+          if (!(vis >> (k & 7) & 1)) continue;
+#pragma unroll
+          for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const size_t i = base + vc_off(p0 + k, d0 + t * 16 + (lane >> 4) * 4 + j, HD);
+              const float v = KVB ? bf_bits2f(((const uint16_t*)a.vc)[i]) : ((const float*)a.vc)[i];
+              if (!(fabsf(v) < INFINITY)) o[t][j] += p * v;
+            }
+        }
       }
     }
     if (KVB) {
@@ -309,17 +341,17 @@ __device__ __forceinline__ void direct_sums(const ShareArgs& a, const QuerySet& 
 }
 
 // sums of query q (of 16) over the waves: dims 16 t + 4 (l / 16) + 0..3 of it, l % 16 = q
-template <int VD>
-__device__ __forceinline__ void join_waves(const WaveSums<VD>& sums, int t, int l, float& M, float& L, f32x4& acc) {
+template <int NW, int VD>
+__device__ __forceinline__ void join_waves(const WaveSums<NW, VD>& sums, int t, int l, float& M, float& L, f32x4& acc) {
   const int q = l & 15;
   M = sums.m[0][q];
 #pragma unroll
-  for (int x = 1; x < SW; ++x) M = fmaxf(M, sums.m[x][q]);
+  for (int x = 1; x < NW; ++x) M = fmaxf(M, sums.m[x][q]);
   const float b = M == -INFINITY ? 0.f : M;
   acc = f32x4{0.f, 0.f, 0.f, 0.f};
   L = 0.f;
 #pragma unroll
-  for (int x = 0; x < SW; ++x) {
+  for (int x = 0; x < NW; ++x) {
     const float f = __builtin_amdgcn_exp2f(sums.m[x][q] - b);
     acc += sums.o[x][t][l] * f;
     L += sums.l[x][q] * f;
@@ -329,8 +361,8 @@ __device__ __forceinline__ void join_waves(const WaveSums<VD>& sums, int t, int 
 // 16 queries over keys without a mask, as chunk `slot` of the partials
 template <int KVB, int HD>
 __device__ void direct_part(const ShareArgs& a, const QuerySet& qs, int win, int k0, int k1, int y, int slot, char* lds) {
-  WaveSums<HD>& sums = *(WaveSums<HD>*)lds;
-  direct_sums<KVB, HD, HD, 0>(a, qs, KeyRange{win, k0, k1, 0}, y, 0, sums);
+  WaveSums<SW, HD>& sums = *(WaveSums<SW, HD>*)lds;
+  direct_sums<KVB, HD, HD, 0>(a, qs, [&] { return KeyRange{win, k0, k1, 0}; }, y, 0, sums);
   const int G = a.n_heads / a.n_kv;
   for (int it = threadIdx.x; it < HD / 16 * 64; it += SW * 64) {
     const int t = it >> 6, l = it & 63, qc = y * 16 + (l & 15);
@@ -374,7 +406,7 @@ template <int HD, int QT>
 constexpr int tile_lds() { return 2 * tile_stage_blocks<HD, QT>() * HD * 128 + SW * 32 * 8; }
 
 template <int HD, int QT>
-__device__ void tile_part(const ShareArgs& a, const QuerySet& qs, int win, int k0, int k1, int y, int slot, char* lds) {
+__device__ void tile_part(const ShareArgs& a, const QuerySet& qs, const ShareGroup& g, int y, int c, char* lds) {
   constexpr int KS = SW / QT, SB = tile_stage_blocks<HD, QT>();
   constexpr int TK = HD / 16, TB = 2 * TK, NPW = SB * TB / SW;
   constexpr int DS = HD / 16, DT = HD / 32;
@@ -385,7 +417,18 @@ __device__ void tile_part(const ShareArgs& a, const QuerySet& qs, int win, int k
   const int qi = (y * QT + qt) * 32 + c32;
   const bool qvalid = qi < qn;
   const int m = qs.row0 + (qvalid ? qi % qs.rows : 0), head = qs.kvh * G + (qvalid ? qi / qs.rows : 0);
-  const size_t base = ((size_t)win * a.n_kv + qs.kvh) * (size_t)a.maxlen * HD * 2;
+  // the queries' loads do not wait for the lengths
+  const float* qrow = a.q + ((size_t)m * a.n_heads + head) * HD + h * 8;
+  F8 qf[DS];
+#pragma unroll
+  for (int ds = 0; ds < DS; ++ds) {
+    qf[ds].a = *(const float4*)(qrow + ds * 16);
+    qf[ds].b = *(const float4*)(qrow + ds * 16 + 4);
+  }
+  const int shared = group_prefix(a, g), per = prefix_chunk(shared, a.p_chunks);
+  const int k0 = c * per, k1 = min(shared, k0 + per), slot = c;
+  if (k0 >= k1) return;
+  const size_t base = ((size_t)g.root * a.n_kv + qs.kvh) * (size_t)a.maxlen * HD * 2;
   const char* kc = (const char*)a.kc + base;
   const char* vc = (const char*)a.vc + base;
   const int blk0 = k0 >> 5, nblk = (k1 - k0) >> 5, stages = (nblk + SB - 1) / SB;
@@ -408,11 +451,10 @@ __device__ void tile_part(const ShareArgs& a, const QuerySet& qs, int win, int k
   };
   load_stage(0);
   const float scale2 = a.scale * 1.44269504088896340736f;   // log2 e
-  const float* qrow = a.q + ((size_t)m * a.n_heads + head) * HD + h * 8;
   bf16x8 qh[DS], ql[DS];
 #pragma unroll
   for (int ds = 0; ds < DS; ++ds) {
-    const float4 x = *(const float4*)(qrow + ds * 16), z = *(const float4*)(qrow + ds * 16 + 4);
+    const float4 x = qf[ds].a, z = qf[ds].b;
     const float f = qvalid ? scale2 : 0.f;
     const float v[8] = {x.x * f, x.y * f, x.z * f, x.w * f, z.x * f, z.y * f, z.z * f, z.w * f};
     u32x4 hi, lo;
@@ -588,7 +630,7 @@ __device__ void append_rows(const ShareArgs& a, int win, int kvh) {
 // (tile_part), or 0: 16 queries on the direct path (fp32 caches)
 template <int KVB, int HD, int QT>
 __global__ __launch_bounds__(SW * 64) void k_share(ShareArgs a) {
-  constexpr int kDirectLds = sizeof(WaveSums<HD>);
+  constexpr int kDirectLds = sizeof(WaveSums<SW, HD>);
   constexpr int kTileLds = QT ? tile_lds<HD, QT ? QT : 8>() : 0;
   __shared__ __align__(16) char lds[kDirectLds > kTileLds ? kDirectLds : kTileLds];
   // ids of one KV head are equal mod n_kv: with eight or a multiple of eight
@@ -601,11 +643,14 @@ __global__ __launch_bounds__(SW * 64) void k_share(ShareArgs a) {
     const ShareGroup& g = a.group[id % a.n_groups];
     id /= a.n_groups;
     const int y = id % a.p_tiles, c = id / a.p_tiles;
-    const int s = group_prefix(a, g), per = prefix_chunk(s, a.p_chunks);
     const QuerySet qs{g.first * a.R, g.count * a.R, kvh};
-    if (c * per >= s || y * (QT ? 32 * QT : 16) >= qs.rows * (a.n_heads / a.n_kv)) return;
-    if constexpr (QT > 0) tile_part<HD, QT>(a, qs, g.root, c * per, min(s, c * per + per), y, c, lds);
-    else direct_part<KVB, HD>(a, qs, g.root, c * per, min(s, c * per + per), y, c, lds);
+    if (y * (QT ? 32 * QT : 16) >= qs.rows * (a.n_heads / a.n_kv)) return;
+    if constexpr (QT > 0) {
+      tile_part<HD, QT>(a, qs, g, y, c, lds);
+    } else {
+      const int s = group_prefix(a, g), per = prefix_chunk(s, a.p_chunks);
+      if (c * per < s) direct_part<KVB, HD>(a, qs, g.root, c * per, min(s, c * per + per), y, c, lds);
+    }
     return;
   }
   id -= n_prefix;
@@ -627,36 +672,49 @@ __global__ __launch_bounds__(SW * 64) void k_share(ShareArgs a) {
 // to the window's last keys and the rows, and joins that with the partials of its
 // queries, in order.  Heads of more than 64 dims are halved: twice the workgroups
 // read the partials, for a second reading of the few keys.
+// What is known without the lengths is loaded before they are: the queries, and
+// the first CB partials (of chunks that may turn out not to exist).
 template <int KVB, int HD>
-__global__ __launch_bounds__(SW * 64) void k_share_last(ShareArgs a) {
+__global__ __launch_bounds__(LW * 64, KVB ? 2 : 1) void k_share_last(ShareArgs a) {
   constexpr int NV = HD > 64 ? 2 : 1, VD = HD / NV, CB = 8;
-  __shared__ __align__(16) WaveSums<VD> sums;
+  static_assert(VD / 16 * 64 <= LW * 64, "a piece of four dims of a query per thread");
+  __shared__ __align__(16) WaveSums<LW, VD> sums;
   int id = blockIdx.x;
   const int kvh = id % a.n_kv;
   id /= a.n_kv;
   const int d0 = id % NV * VD;
   id /= NV;
   const int win = id % a.B, y = id / a.B;
-  const int s = window_prefix(a, win);
-  const int len = min(a.f.lens[a.window0 + win], a.maxlen - a.R);
-  const int e = own_end(s, len);
+  const int G = a.n_heads / a.n_kv;
+  // this thread's piece of the result
+  const int t = threadIdx.x >> 6, l = threadIdx.x & 63;
+  const int qc = min(y * 16 + (l & 15), G * a.R - 1);
+  const int m = win * a.R + qc % a.R, head = kvh * G + qc / a.R, d = d0 + t * 16 + (l >> 4) * 4;
+  const size_t rows = (size_t)a.B * a.R * a.n_heads, r = (size_t)m * a.n_heads + head;
+  const bool piece = t < VD / 16;
+  float2 ml[CB];
+  f32x4 o[CB];
+#pragma unroll
+  for (int j = 0; j < CB; ++j) {
+    const size_t slot = (size_t)min(j, a.p_chunks + a.t_chunks - 1) * rows + r;
+    ml[j] = a.part_ml[slot];
+    o[j] = *(const f32x4*)(a.part_o + slot * HD + (piece ? d : 0));
+  }
+  int s, e, len;
+  direct_sums<KVB, HD, VD, 1>(a, QuerySet{win * a.R, a.R, kvh}, [&] {
+    s = window_prefix(a, win);
+    len = min(a.f.lens[a.window0 + win], a.maxlen - a.R);
+    e = own_end(s, len);
+    return KeyRange{a.window0 + win, e, len + a.R, len};
+  }, y, d0, sums);
+  if (!piece || y * 16 + (l & 15) >= G * a.R) return;
   const int np = s ? (s + prefix_chunk(s, a.p_chunks) - 1) / prefix_chunk(s, a.p_chunks) : 0;
   const int nc = np + (e > s ? (e - s + own_chunk(e - s, a.t_chunks) - 1) / own_chunk(e - s, a.t_chunks) : 0);
-  const int G = a.n_heads / a.n_kv;
-  const size_t rows = (size_t)a.B * a.R * a.n_heads;
-  direct_sums<KVB, HD, VD, 1>(a, QuerySet{win * a.R, a.R, kvh}, KeyRange{a.window0 + win, e, len + a.R, len}, y, d0, sums);
-  // the 64 pieces of four dims of each 16 dims on one wave
-  for (int it = threadIdx.x; it < VD / 16 * 64; it += SW * 64) {
-    const int t = it >> 6, l = it & 63, qc = y * 16 + (l & 15);
-    if (qc >= G * a.R) continue;
-    const int m = win * a.R + qc % a.R, head = kvh * G + qc / a.R, d = d0 + t * 16 + (l >> 4) * 4;
-    const size_t r = (size_t)m * a.n_heads + head;
-    float M, L;
-    f32x4 acc;
-    join_waves(sums, t, l, M, L, acc);
-    for (int c0 = 0; c0 < nc; c0 += CB) {
-      float2 ml[CB];
-      f32x4 o[CB];
+  float M, L;
+  f32x4 acc;
+  join_waves(sums, t, l, M, L, acc);
+  for (int c0 = 0; c0 < nc; c0 += CB) {
+    if (c0 || np < min(nc, CB)) {   // else they are the partials loaded above
 #pragma unroll
       for (int j = 0; j < CB; ++j) {
         const int c = min(c0 + j, nc - 1);
@@ -664,27 +722,28 @@ __global__ __launch_bounds__(SW * 64) void k_share_last(ShareArgs a) {
         ml[j] = a.part_ml[slot];
         o[j] = *(const f32x4*)(a.part_o + slot * HD + d);
       }
-      float Mn = M;
-#pragma unroll
-      for (int j = 0; j < CB; ++j) Mn = fmaxf(Mn, ml[j].x);
-      const float b = Mn == -INFINITY ? 0.f : Mn;
-      const float f0 = __builtin_amdgcn_exp2f(M - b);
-      L *= f0;
-      acc *= f0;
-      M = Mn;
-#pragma unroll
-      for (int j = 0; j < CB; ++j)
-        if (c0 + j < nc) {
-          const float f = __builtin_amdgcn_exp2f(ml[j].x - b);
-          L += ml[j].y * f;
-          acc += o[j] * f;
-        }
     }
-    const float inv = 1.0f / L;
-    const float y4[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
-    if (a.out_rows) *(float4*)(a.out_rows + r * HD + d) = float4{y4[0], y4[1], y4[2], y4[3]};
-    else pack_store4(a.out, a.wtype, m, head * HD + d, y4);
+    float Mn = M;
+#pragma unroll
+    for (int j = 0; j < CB; ++j)
+      if (c0 + j < nc) Mn = fmaxf(Mn, ml[j].x);
+    const float b = Mn == -INFINITY ? 0.f : Mn;
+    const float f0 = __builtin_amdgcn_exp2f(M - b);
+    L *= f0;
+    acc *= f0;
+    M = Mn;
+#pragma unroll
+    for (int j = 0; j < CB; ++j)
+      if (c0 + j < nc) {
+        const float f = __builtin_amdgcn_exp2f(ml[j].x - b);
+        L += ml[j].y * f;
+        acc += o[j] * f;
+      }
   }
+  const float inv = 1.0f / L;
+  const float y4[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+  if (a.out_rows) *(float4*)(a.out_rows + r * HD + d) = float4{y4[0], y4[1], y4[2], y4[3]};
+  else pack_store4(a.out, a.wtype, m, head * HD + d, y4);
 }
 
 template <int KVB, int HD, int QT>
@@ -694,7 +753,7 @@ hipError_t launch_shared_qt(const ShareArgs& a, hipStream_t s) {
   if (wgs) hipLaunchKernelGGL((k_share<KVB, HD, QT>), dim3((unsigned)wgs), dim3(SW * 64), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_share_last<KVB, HD>), dim3((unsigned)a.B * a.n_kv * a.t_tiles * (HD > 64 ? 2 : 1)), dim3(SW * 64),
+  hipLaunchKernelGGL((k_share_last<KVB, HD>), dim3((unsigned)a.B * a.n_kv * a.t_tiles * (HD > 64 ? 2 : 1)), dim3(LW * 64),
                      0, s, a);
   return hipGetLastError();
 }
