@@ -646,8 +646,7 @@ struct SharePlan {
 
 // The host knows which window each was forked from; how much of it is still
 // shared is known on the device when the attention runs, so the partition goes
-// by the cache's capacity.  About one workgroup per CU for the prefix, and two
-// for the windows' own keys, which are mostly short.
+// by the cache's capacity.
 SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, int R) {
   SharePlan p;
   ShareArgs& a = p.a;
@@ -673,8 +672,14 @@ SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, 
   const int G = m->hq / m->hkv;
   a.p_tile = share_tile(m->kvb, G * R * most);
   a.t_tiles = cdiv(G * R, 16);
-  a.t_chunks = std::min(std::max(1, 512 / (B * m->hkv * a.t_tiles)), cdiv(kv->max_len, 256));
+  // a window that shares nothing is read in chunks for two rounds of workgroups;
+  // forked ones have little of their own, and most of these workgroups only
+  // cache the rows (6 x 7 rows over 1024 shared keys, 13B: 17.6 us with 480 of
+  // them, 16.7 with 240)
+  a.t_chunks = std::min(std::max(1, (a.n_groups ? 128 : 512) / (B * m->hkv * a.t_tiles)), cdiv(kv->max_len, 256));
   if (a.n_groups) {
+    // a CU for each part of the prefix (31 instead of 32 chunks, to leave CUs
+    // for those workgroups: 83 instead of 78 us at 32768 keys)
     a.p_tiles = cdiv(G * R * most, a.p_tile);
     a.p_chunks = std::min(std::max(1, 256 / (a.n_groups * m->hkv * a.p_tiles)), cdiv(kv->max_len, 128));
   }

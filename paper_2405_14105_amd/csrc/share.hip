@@ -27,7 +27,6 @@ namespace {
 constexpr int SW = 8;                  // waves per workgroup of the first launch
 constexpr int LW = 4;                  // and of the second
 constexpr int kMinShared = 128;        // a shorter shared prefix is read by each window
-constexpr int kMinPrefixChunk = 128;   // keys per workgroup at least
 constexpr int kLast = 256;             // cached keys that the second launch takes at most
 constexpr int kOwnChunk = SW * 32;     // keys of a window's own per workgroup of the first launch: a multiple of this
 
@@ -54,9 +53,13 @@ __device__ __forceinline__ int window_prefix(const ShareArgs& a, int win) {
     if (win >= a.group[g].first && win < a.group[g].first + a.group[g].count) return group_prefix(a, a.group[g]);
   return 0;
 }
-// keys per chunk: at most `most` chunks
-__device__ __forceinline__ int prefix_chunk(int s, int most) {
-  return max(kMinPrefixChunk, ((s + most - 1) / most + 63) & ~63);
+// keys per chunk of a prefix: p_chunks chunks at most, of 128 keys at least, or
+// 192 where a part has up to 256 queries and the prefix over 2048 keys: a chunk
+// leaves HD * 4 bytes per query, which are read again (8B: 8 x 8 rows over 4096 keys
+// 40.6 us with 32 chunks of 128, 36.8 with 22 of 192; 7 x 6 over 2048 26.1 with 16
+// of 128, 28.2 with 11 of 192)
+__device__ __forceinline__ int prefix_chunk(const ShareArgs& a, int s) {
+  return max(a.p_tile > 128 && s > 2048 ? 192 : 128, ((s + a.p_chunks - 1) / a.p_chunks + 63) & ~63);
 }
 __device__ __forceinline__ int own_chunk(int keys, int most) {
   return ((keys + most - 1) / most + kOwnChunk - 1) / kOwnChunk * kOwnChunk;
@@ -398,8 +401,14 @@ __device__ __forceinline__ f32x16 mfma32_bf16(const bf16x8& a, const bf16x8& b, 
 // LDS, so that the 16 rows a fragment read takes the same piece of lie in 16
 // different groups of banks.
 // Queries (times scale and log2 e) and probabilities are hi + lo bf16, as in
-// the window attention; the running maximum moves only when a score is 2^8 above
-// it, so most blocks rescale nothing.
+// the window attention, which leaves 2^-18 of each: twice the products for an
+// error of 5e-6 of the output where fp32 sums leave 1e-6.  The running maximum
+// moves only when a score is 2^8 above it, so most blocks rescale nothing.
+// 256 queries over 32768 keys (8 KV heads of 128): 77 us, 0.9 PFLOP/s of these
+// products, where a library product of 8192^3 reaches 1.2 on the same card; 40 KV
+// heads with 42 queries over 8191 keys: 43 us, 5.5 TB/s once running, 16 us of it
+// launch, first loads, the waves' join and the partials' stores.  Four waves with
+// 64 queries each, a SIMD to themselves: 93 and 70 us.
 template <int HD, int QT>
 constexpr int tile_stage_blocks() { return SW / QT < 2 ? 2 : SW / QT; }
 template <int HD, int QT>
@@ -425,7 +434,7 @@ __device__ void tile_part(const ShareArgs& a, const QuerySet& qs, const ShareGro
     qf[ds].a = *(const float4*)(qrow + ds * 16);
     qf[ds].b = *(const float4*)(qrow + ds * 16 + 4);
   }
-  const int shared = group_prefix(a, g), per = prefix_chunk(shared, a.p_chunks);
+  const int shared = group_prefix(a, g), per = prefix_chunk(a, shared);
   const int k0 = c * per, k1 = min(shared, k0 + per), slot = c;
   if (k0 >= k1) return;
   const size_t base = ((size_t)g.root * a.n_kv + qs.kvh) * (size_t)a.maxlen * HD * 2;
@@ -472,33 +481,21 @@ __device__ void tile_part(const ShareArgs& a, const QuerySet& qs, const ShareGro
   const int koff = (key >> 4) * 1024 + (key & 15) * 64 + (h ^ (key >> 2 & 3)) * 16;
   const int voff = TK * 1024 + (c32 >> 4) * 1024 + (c32 & 15) * 64 + (h ^ (c32 >> 2 & 3)) * 16;
 
-  // NB blocks of 32 keys at once, at p and TB KB apart: two independent chains
-  // of matrix instructions either way
-  constexpr int NB = 1;
-  auto blocks = [&](const char* p, auto full) {
-    constexpr int N = decltype(full)::value;
-    f32x16 s[2];
+  // one block of 32 keys
+  auto block = [&](const char* p) {
+    f32x16 s, s2;   // two independent chains
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
+    for (int i = 0; i < 16; ++i) s[i] = s2[i] = 0.f;
 #pragma unroll
     for (int ds = 0; ds < DS; ++ds) {
-      const int at = (koff ^ (ds & 1) * 32) + (ds >> 1) * 2048;
-      const bf16x8 k0 = as_bf16x8(*(const u32x4*)(p + at));
-      if constexpr (N == 2) {
-        const bf16x8 k1 = as_bf16x8(*(const u32x4*)(p + TB * 1024 + at));
-        s[0] = mfma32_bf16(k0, qh[ds], s[0]);
-        s[1] = mfma32_bf16(k1, qh[ds], s[1]);
-        s[0] = mfma32_bf16(k0, ql[ds], s[0]);
-        s[1] = mfma32_bf16(k1, ql[ds], s[1]);
-      } else {
-        s[0] = mfma32_bf16(k0, qh[ds], s[0]);
-        s[1] = mfma32_bf16(k0, ql[ds], s[1]);
-      }
+      const bf16x8 kf = as_bf16x8(*(const u32x4*)(p + (koff ^ (ds & 1) * 32) + (ds >> 1) * 2048));
+      s = mfma32_bf16(kf, qh[ds], s);
+      s2 = mfma32_bf16(kf, ql[ds], s2);
     }
-    if constexpr (N == 1) s[0] += s[1];
-    float mx = s[0][0];
+    s += s2;
+    float mx = s[0];
 #pragma unroll
-    for (int i = 1; i < 16 * N; ++i) mx = fmaxf(mx, s[i >> 4][i & 15]);
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
     mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
     if (__ballot(mx > mrun + 8.f)) {
@@ -510,27 +507,33 @@ __device__ void tile_part(const ShareArgs& a, const QuerySet& qs, const ShareGro
       for (int t = 0; t < DT; ++t) o[t] *= alpha;
     }
     const float b = mrun == -INFINITY ? 0.f : mrun;
-    float ls[2] = {0.f, 0.f};
+    float pv[2][8], ls[2] = {0.f, 0.f};
+    auto weight = [&](int half, int i) {
+      pv[half][i] = __builtin_amdgcn_exp2f(s[half * 8 + i] - b);
+      ls[i & 1] += pv[half][i];
+    };
 #pragma unroll
-    for (int c = 0; c < 2 * N; ++c) {   // 16 keys
-      float pv[8];
+    for (int i = 0; i < 8; ++i) weight(0, i);
+    // the second 16 keys' weights between the first's matrix instructions
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        pv[i] = __builtin_amdgcn_exp2f(s[c >> 1][(c & 1) * 8 + i] - b);
-        ls[i & 1] += pv[i];
-      }
+    for (int half = 0; half < 2; ++half) {
       u32x4 hi, lo;
-      split8(pv, hi, lo);
+      split8(pv[half], hi, lo);
       const bf16x8 ph = as_bf16x8(hi), pl = as_bf16x8(lo);
       bf16x8 vf[DT];
 #pragma unroll
-      for (int t = 0; t < DT; ++t)
-        vf[t] = as_bf16x8(*(const u32x4*)(p + (c >> 1) * (TB * 1024) + (voff ^ (c & 1) * 32) + t * 2048));
+      for (int t = 0; t < DT; ++t) vf[t] = as_bf16x8(*(const u32x4*)(p + (voff ^ half * 32) + t * 2048));
+  #pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        o[t] = mfma32_bf16(vf[t], ph, o[t]);
+        if (half == 0) {
 #pragma unroll
-      for (int t = 0; t < DT; ++t) o[t] = mfma32_bf16(vf[t], ph, o[t]);
+          for (int i = t * 8 / DT; i < (t + 1) * 8 / DT; ++i) weight(1, i);
+        }
+      }
 #pragma unroll
       for (int t = 0; t < DT; ++t) o[t] = mfma32_bf16(vf[t], pl, o[t]);
-    }
+      }
     lrun += ls[0] + ls[1];
   };
 
@@ -539,7 +542,7 @@ __device__ void tile_part(const ShareArgs& a, const QuerySet& qs, const ShareGro
     const char* p = lds + (st & 1) * (SB * TB * 1024);
 #pragma unroll
     for (int i = 0; i < SB; i += KS)
-      if (live && st * SB + i + ks < nblk) blocks(p + (i + ks) * (TB * 1024), std::integral_constant<int, 1>{});
+      if (live && st * SB + i + ks < nblk) block(p + (i + ks) * (TB * 1024));
   };
   store_stage(0);
   __syncthreads();
@@ -648,7 +651,7 @@ __global__ __launch_bounds__(SW * 64) void k_share(ShareArgs a) {
     if constexpr (QT > 0) {
       tile_part<HD, QT>(a, qs, g, y, c, lds);
     } else {
-      const int s = group_prefix(a, g), per = prefix_chunk(s, a.p_chunks);
+      const int s = group_prefix(a, g), per = prefix_chunk(a, s);
       if (c * per < s) direct_part<KVB, HD>(a, qs, g.root, c * per, min(s, c * per + per), y, c, lds);
     }
     return;
@@ -708,7 +711,7 @@ __global__ __launch_bounds__(LW * 64, KVB ? 2 : 1) void k_share_last(ShareArgs a
     return KeyRange{a.window0 + win, e, len + a.R, len};
   }, y, d0, sums);
   if (!piece || y * 16 + (l & 15) >= G * a.R) return;
-  const int np = s ? (s + prefix_chunk(s, a.p_chunks) - 1) / prefix_chunk(s, a.p_chunks) : 0;
+  const int np = s ? (s + prefix_chunk(a, s) - 1) / prefix_chunk(a, s) : 0;
   const int nc = np + (e > s ? (e - s + own_chunk(e - s, a.t_chunks) - 1) / own_chunk(e - s, a.t_chunks) : 0);
   float M, L;
   f32x4 acc;
