@@ -431,6 +431,7 @@ hipError_t launch_fork_cut(const ForkState& f, int window, int new_len, hipStrea
 // Attention of B windows' rows, the prefix that windows forked from one window
 // share read once for all of them (share.hip).
 constexpr int kMaxForkGroups = kMaxRows / 2;
+constexpr int kMinShared = 128;   // a shorter shared prefix is read by each window
 struct ShareGroup {
   int first, count;     // windows of the call
   int root;             // the window forked from

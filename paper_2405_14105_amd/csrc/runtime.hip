@@ -122,6 +122,7 @@ struct dsi_model {
   // whether one-row-tile forwards on single-window caches use them
   RingCfg rc_qkv, rc_o, rc_gu, rc_down, rc_head;
   bool use_ring = true;
+  int share = -1;               // forwards read shared prefixes once: 0 never, 1 always, -1 by size
   void* embed = nullptr;
   float* final_norm = nullptr;
   void* lm_head = nullptr;
@@ -188,6 +189,7 @@ struct dsi_kv {
   int* lens = nullptr;             // [3][n_windows]: lengths, then ForkState's root and shared
   std::vector<long long> hi, lo;   // host bounds on each window's length
   std::vector<int> root;           // the window each was last forked from, or -1
+  std::vector<long long> shared;   // host bound on what the two still have in common
   size_t win_elems = 0;            // elements of one (layer, window) of K (= of V)
   ForkState forks() const { return ForkState{lens, lens + n_windows, lens + 2 * n_windows, n_windows}; }
 };
@@ -641,12 +643,27 @@ dsi_status plan_attention(dsi_model* m, dsi_kv* kv, int window0, int B, int R, A
 struct SharePlan {
   ShareArgs a{};        // groups, tiles and chunks; the rest by share_args
   size_t parts = 0;     // partial rows
-  bool any() const { return a.n_groups > 0; }
+  size_t saved = 0;     // bytes of keys and values that need not be read again
 };
+
+// A forward reads a shared prefix once where that saves so much in a layer; below,
+// the window kernels are faster, whose workgroups are smaller and more (us a
+// layer, by themselves and shared.  8B, 7 windows of 6 rows: 2048 positions, 50
+// MB, 28.1 and 28.7; 4096 46.7 and 33.8; 32768 219 and 79; 2 of 11: 8192, 34 MB,
+// 32.5 and 35.5; 3 of 1: 4096, 34 MB, 21.5 and 25.2; 8192 36.8 and 27.7.  13B, 6 of
+// 7: 512, 52 MB, 17.6 and 23.3; 1024 27.4 and 26.5; 2048 61 and 30.  1B, 4 of 6:
+// 8192, 50 MB, 22.7 and 26.9; 32768 71 and 40)
+constexpr size_t kShareSaves = (size_t)64 << 20;
 
 // The host knows which window each was forked from; how much of it is still
 // shared is known on the device when the attention runs, so the partition goes
 // by the cache's capacity.
+// a window's rows from len on may change from now on (fork_cut, on the device)
+void cut_shared(dsi_kv* kv, int window, long long len) {
+  for (int w = 0; w < kv->n_windows; ++w)
+    if (w == window || kv->root[w] == window) kv->shared[w] = std::min(kv->shared[w], len);
+}
+
 SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, int R) {
   SharePlan p;
   ShareArgs& a = p.a;
@@ -655,7 +672,7 @@ SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, 
   a.R = R;
   auto run = [&](int i, int r) {   // windows from i on that are r or were forked from it
     int j = i;
-    while (j < B && (window0 + j == r || kv->root[window0 + j] == r)) ++j;
+    while (j < B && (window0 + j == r || (kv->root[window0 + j] == r && kv->shared[window0 + j] >= kMinShared))) ++j;
     return j - i;
   };
   int most = 0;
@@ -666,6 +683,10 @@ SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, 
     if (n > 1) {
       a.group[a.n_groups++] = ShareGroup{i, n, r};
       most = std::max(most, n);
+      long long common = kv->max_len;
+      for (int j = i; j < i + n; ++j)
+        common = std::min(common, window0 + j == r ? kv->hi[r] : kv->shared[window0 + j]);
+      p.saved += (size_t)(n - 1) * common * 2 * m->kvdim * m->kvesz;
     }
     i += n;
   }
@@ -685,6 +706,11 @@ SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, 
   }
   p.parts = (size_t)(a.p_chunks + a.t_chunks) * B * R * m->hq;
   return p;
+}
+
+// whether a forward takes the plan
+bool share_forward(const dsi_model* m, const SharePlan& p) {
+  return p.a.n_groups > 0 && (m->share == 1 || (m->share < 0 && p.saved >= kShareSaves));
 }
 
 ShareArgs share_args(const dsi_model* m, const dsi_kv* kv, const SharePlan& p, int layer, const float* q) {
@@ -782,7 +808,7 @@ dsi_status run_forward(dsi_model* m, dsi_kv* kv, const AttnPlan& ap, int window0
     aa.wtype = m->wtype;
     aa.anc = anc;
     aa.waves = ap.waves;
-    if (shared && shared->any()) {
+    if (shared) {
       ShareArgs sa = share_args(m, kv, *shared, l, m->qbuf);
       sa.anc = anc;
       sa.out = m->pk_q;
@@ -1271,6 +1297,8 @@ dsi_status dsi_model_create(const dsi_config* cfg, void* stream, dsi_model** out
   m->Nb_head = cdiv(m->V, 16);
   m->G_gu = gemm_wgroup(m->wtype, EPI_SILU, m->Nb_gu);
   m->G_head = gemm_wgroup(m->wtype, EPI_STORE, m->Nb_head);
+  const char* sh = getenv("DSI_SHARE");
+  m->share = sh && sh[0] == '0' ? 0 : sh && sh[0] == '1' ? 1 : -1;
   const char* rg = getenv("DSI_RING");
   m->use_ring = !(rg && rg[0] == '0');
   ring_config(m->wtype, EPI_QKV, m->Nb_qkv, m->Kb_d, 1, &m->rc_qkv);
@@ -1496,6 +1524,7 @@ static dsi_status kv_new(dsi_model* m, int n_windows, int max_len, dsi_kv** out)
   kv->hi.assign(n_windows, 0);
   kv->lo.assign(n_windows, 0);
   kv->root.assign(n_windows, -1);
+  kv->shared.assign(n_windows, 0);
   *out = kv;
   return DSI_OK;
 }
@@ -1626,7 +1655,8 @@ dsi_status dsi_verify(dsi_model* m, dsi_kv* kv, const dsi_verify_args* a, int32_
   AttnPlan ap;
   DSI_TRY(plan_attention(m, kv, a->window0, B, k + 1, &ap));
   const SharePlan sp = plan_shared(m, kv, a->window0, B, k + 1);
-  if (sp.any()) DSI_TRY(ensure_attention(m, sp.parts));
+  const bool share = share_forward(m, sp);
+  if (share) DSI_TRY(ensure_attention(m, sp.parts));
   m->last_window0 = a->window0;
   m->last_B = B;
   m->last_R = k + 1;
@@ -1648,7 +1678,7 @@ dsi_status dsi_verify(dsi_model* m, dsi_kv* kv, const dsi_verify_args* a, int32_
   va.err = m->err;
   verify_bind_workspace(va, m->vws, B * (k + 1), B, m->V);
   auto launches = [&]() -> dsi_status {
-    DSI_TRY(run_forward(m, kv, ap, a->window0, B, k + 1, a->d_tokens, logits, 0, a->d_hidden_out, nullptr, nullptr, &sp));
+    DSI_TRY(run_forward(m, kv, ap, a->window0, B, k + 1, a->d_tokens, logits, 0, a->d_hidden_out, nullptr, nullptr, share ? &sp : nullptr));
     Prof p(m, DSI_K_VERIFY);
     HIP_TRY(launch_verify(va, m->stream));
     return DSI_OK;
@@ -1667,7 +1697,7 @@ dsi_status dsi_verify(dsi_model* m, dsi_kv* kv, const dsi_verify_args* a, int32_
         (uint64_t)kv->n_windows, (uint64_t)kv->max_len, (uint64_t)kv->maxlen_pad,
         (uint64_t)ap.n_qtiles, (uint64_t)ap.chunk, (uint64_t)ap.n_chunks, (uint64_t)ap.waves,
         (uint64_t)(uintptr_t)m->attn_o, (uint64_t)(uintptr_t)m->attn_ml};
-    share_key(sp, &key);
+    if (share) share_key(sp, &key);
     DSI_TRY(replay_or_capture(m, key, launches));
   } else {
     DSI_TRY(launches());
@@ -1700,7 +1730,8 @@ dsi_status dsi_verify_tree(dsi_model* m, dsi_kv* kv, const dsi_tree_args* a, int
   AttnPlan ap;
   DSI_TRY(plan_attention(m, kv, a->window0, B, R, &ap));
   const SharePlan sp = plan_shared(m, kv, a->window0, B, R);
-  if (sp.any()) DSI_TRY(ensure_attention(m, sp.parts));
+  const bool share = share_forward(m, sp);
+  if (share) DSI_TRY(ensure_attention(m, sp.parts));
   m->last_window0 = a->window0;
   m->last_B = B;
   m->last_R = R;
@@ -1735,7 +1766,7 @@ dsi_status dsi_verify_tree(dsi_model* m, dsi_kv* kv, const dsi_tree_args* a, int
   const size_t layer_elems = (size_t)kv->n_windows * kv->win_elems;
   auto launches = [&]() -> dsi_status {
     HIP_TRY(launch_tree_prep(ta, m->stream));
-    DSI_TRY(run_forward(m, kv, ap, a->window0, B, R, a->d_tokens, logits, 0, nullptr, m->tdepth, m->tanc, &sp));
+    DSI_TRY(run_forward(m, kv, ap, a->window0, B, R, a->d_tokens, logits, 0, nullptr, m->tdepth, m->tanc, share ? &sp : nullptr));
     Prof p(m, DSI_K_VERIFY);
     HIP_TRY(launch_verify_rowstats(va, m->stream));
     HIP_TRY(launch_tree_decide(ta, m->stream));
@@ -1753,7 +1784,7 @@ dsi_status dsi_verify_tree(dsi_model* m, dsi_kv* kv, const dsi_tree_args* a, int
         (uint64_t)kv->n_windows, (uint64_t)kv->max_len, (uint64_t)kv->maxlen_pad,
         (uint64_t)ap.n_qtiles, (uint64_t)ap.chunk, (uint64_t)ap.n_chunks, (uint64_t)ap.waves,
         (uint64_t)(uintptr_t)m->attn_o, (uint64_t)(uintptr_t)m->attn_ml};
-    share_key(sp, &key);
+    if (share) share_key(sp, &key);
     DSI_TRY(replay_or_capture(m, key, launches));
   } else {
     DSI_TRY(launches());
@@ -1915,8 +1946,9 @@ dsi_status dsi_kv_fork(dsi_kv* kv, int32_t src, int32_t window0, int32_t n_windo
   a.err = m->err;
   (void)capturing(kv->m);
   HIP_TRY(launch_kv_fork(a, len < 0 ? (int)kv->hi[src] : len, m->stream));
+  for (int w = window0; w < window0 + n_windows; ++w) cut_shared(kv, w, 0);
   for (int w = window0; w < window0 + n_windows; ++w) {
-    kv->hi[w] = len < 0 ? kv->hi[src] : (long long)len;
+    kv->hi[w] = kv->shared[w] = len < 0 ? kv->hi[src] : (long long)len;
     kv->lo[w] = 0;
     kv->root[w] = src;
   }
@@ -2014,6 +2046,7 @@ dsi_status dsi_kv_rollback(dsi_kv* kv, int32_t window, int32_t new_len) {
   HIP_TRY(launch_kv_rollback(kv->forks(), window, new_len, kv->m->err, kv->m->stream));
   kv->hi[window] = new_len;
   kv->lo[window] = std::min(kv->lo[window], (long long)new_len);
+  cut_shared(kv, window, new_len);
   return DSI_OK;
 }
 
@@ -2156,7 +2189,10 @@ static dsi_status kv_copy(dsi_kv* kv, int32_t window, int32_t layer, int32_t len
   dsi_model* m = kv->m;
   if (window < 0 || window >= kv->n_windows || layer < 0 || layer >= m->L || len < 0 || len > kv->max_len)
     return fail(DSI_EINVAL, "bad window / layer / len");
-  if (to_cache) HIP_TRY(launch_fork_cut(kv->forks(), window, 0, m->stream));
+  if (to_cache) {
+    HIP_TRY(launch_fork_cut(kv->forks(), window, 0, m->stream));
+    cut_shared(kv, window, 0);
+  }
   HIP_TRY(launch_kv_copy(to_cache, m->kvb, kv_ptr(kv, kv->k, layer, window), kv_ptr(kv, kv->v, layer, window),
                          m->hkv, m->hd, kv->maxlen_pad, len, dk, dv, m->stream));
   return DSI_OK;
@@ -2177,6 +2213,7 @@ dsi_status dsi_kv_set_length(dsi_kv* kv, int32_t window, int32_t len) {
     return fail(DSI_EINVAL, "bad window / len");
   HIP_TRY(launch_kv_set(kv->forks(), window, len, kv->m->stream));
   kv->hi[window] = kv->lo[window] = len;
+  cut_shared(kv, window, len);
   return DSI_OK;
 }
 

@@ -26,7 +26,6 @@ namespace {
 
 constexpr int SW = 8;                  // waves per workgroup of the first launch
 constexpr int LW = 4;                  // and of the second
-constexpr int kMinShared = 128;        // a shorter shared prefix is read by each window
 constexpr int kLast = 256;             // cached keys that the second launch takes at most
 constexpr int kOwnChunk = SW * 32;     // keys of a window's own per workgroup of the first launch: a multiple of this
 

@@ -168,6 +168,47 @@ class DsiExecutor:
 
 
 @dataclasses.dataclass
+class Scores:
+    logprob: list         # per continuation: log p of each of its tokens
+    entropy: list         # per continuation: entropy of the distribution each was drawn from, in nats
+    top_ids: list         # per continuation and token: the n_top most probable tokens there
+    top_logprobs: list
+
+
+def score_continuations(target: int, kv: int, src: int, window0: int, w0: int, continuations: list, vocab: int,
+                        temperature: float = 1.0, n_top: int = 0) -> Scores:
+    """Log probabilities of several continuations of one prompt under the target
+    (reranking drafts, best-of-n).  Window `src` of the cache holds the prompt up
+    to w0, its last token, which is not cached; windows window0 .. are scratch,
+    one per continuation, and hold the prompt afterwards.  The prompt's cache is
+    forked into them (dsi_kv_fork), all continuations run in one forward that
+    reads the shared prefix once (dsi_verify), and their tokens are scored from
+    its logits (dsi_logprobs).  len(continuations) * (1 + the longest one's
+    length) <= DSI_MAX_ROWS; shorter ones are padded."""
+    B, k = len(continuations), max((len(c) for c in continuations), default=0)
+    if B < 1 or B * (k + 1) > dsi.DSI_MAX_ROWS:
+        raise ValueError("need 1 <= continuations * (longest + 1) <= DSI_MAX_ROWS")
+    dev = torch.device("cuda:0")
+    tokens = torch.tensor([[w0, *c] + [0] * (k - len(c)) for c in continuations], dtype=torch.int32, device=dev)
+    # row i predicts token i of its continuation; -1: no token there
+    targets = torch.tensor([[*c] + [-1] * (k + 1 - len(c)) for c in continuations], dtype=torch.int32, device=dev)
+    rows = B * (k + 1)
+    n = torch.zeros((2, B), dtype=torch.int32, device=dev)
+    logits = torch.empty((rows, vocab), dtype=torch.float32, device=dev)
+    lp, ent = (torch.empty((B, k + 1), dtype=torch.float32, device=dev) for _ in range(2))
+    ids = torch.empty((B, k + 1, n_top), dtype=torch.int32, device=dev)
+    tops = torch.empty((B, k + 1, n_top), dtype=torch.float32, device=dev)
+    ws = torch.empty(dsi.dsi_logprobs_workspace(rows, vocab, n_top), dtype=torch.uint8, device=dev)
+    dsi.dsi_kv_fork(kv, src, window0, B)
+    dsi.dsi_verify(target, kv, window0, B, k, tokens, None, None, n[0], n[1], 1.0, dsi.DSI_GREEDY, False, logits)
+    dsi.dsi_sync(target)                             # the scoring runs on the current stream
+    dsi.dsi_logprobs(torch.cuda.current_stream().cuda_stream, rows, vocab, logits, targets, n_top, lp, ent,
+                     ids if n_top else None, tops if n_top else None, ws, ws.numel(), temperature)
+    cut = lambda t: [x[:len(c)].tolist() for x, c in zip(t.cpu(), continuations)]
+    return Scores(cut(lp), cut(ent), cut(ids), cut(tops))
+
+
+@dataclasses.dataclass
 class TreeRun:
     tokens: list          # the N generated tokens (after w0)
     forwards: int         # target forwards (one tree verification each)

@@ -290,8 +290,9 @@ def test_fork_beyond_the_source_is_reported(dev):
 
 @pytest.mark.parametrize("name", ["tiny", "gqa_hd64", "mha_hd128"])
 @pytest.mark.parametrize("prefix", [100, 200, 517])
-def test_verify_of_forked_windows(dev, name, prefix):
-    """Logits, decisions and cache rows of forked windows against each window run by itself."""
+def test_verify_of_forked_windows(dev, name, prefix, monkeypatch):
+    """Logits and decisions of forked windows against each window run by itself."""
+    monkeypatch.setenv("DSI_SHARE", "1")
     shape, k, B = S.SHAPES[name], 4, 3
     rng = np.random.default_rng(prefix)
     prompt = rng.integers(0, shape.vocab, prefix)
@@ -324,8 +325,23 @@ def test_verify_of_forked_windows(dev, name, prefix):
         assert np.abs(np.concatenate(t1) - t2).max() <= bound
 
 
-def test_verify_replays_of_forked_windows(dev):
+def test_verify_of_a_long_shared_prefix(dev):
+    """Long enough to be read once without being told."""
+    shape, B = S.SHAPES["tiny"], 8
+    rng = np.random.default_rng(1)
+    n = (64 << 20) // (7 * 2 * shape.n_kv_heads * shape.head_dim * 4) + 40
+    toks = rng.integers(0, shape.vocab, (B, 2))
+    with Rig(shape, 0, B, n + 10) as rig:
+        rig.prefill(0, rng.integers(0, shape.vocab, n))
+        dsi.dsi_kv_fork(rig.kv, 0, 1, B - 1)
+        alone = np.concatenate([rig.verify(w, toks[w:w + 1], mode=dsi.DSI_GREEDY, commit=False)["logits"] for w in range(B)])
+        both = rig.verify(0, toks, mode=dsi.DSI_GREEDY, commit=False)["logits"]
+        assert not np.array_equal(alone, both) and np.abs(alone - both).max() <= 2e-4
+
+
+def test_verify_replays_of_forked_windows(dev, monkeypatch):
     """The recorded step is not replayed for another fork, and reads lengths and sharing as they are then."""
+    monkeypatch.setenv("DSI_SHARE", "1")
     shape = S.SHAPES["tiny"]
     stream = torch.cuda.Stream()
     rng = np.random.default_rng(5)
@@ -358,3 +374,90 @@ def test_verify_replays_of_forked_windows(dev):
         dsi.dsi_kv_fork(rig.kv, 2, 0, 2)         # another root for the same windows
         for _ in range(2):
             step()
+
+
+# ------------------------------------------------------------------- together
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_decoding_from_a_fork(dev, kind):
+    """A prompt forked into four windows that then go their own ways, several rows and one at a time."""
+    with Cache(8, 2, 64, kind, 4, 700, layers=2) as c:
+        lens = forked(c, 0, range(4), 517, [0, 0, 0, 0])
+        for rows in (1, 5, 1, 1, 90, 1):
+            for layer in range(2):
+                q, k, v = c.rows(4 * rows)
+                out = c.attend(0, 4, rows, q, k, v, layer, commit=layer == 1)
+                check(c, out, 0, rows, lens, q, k, v, layer)
+            lens = [n + rows for n in lens]
+            assert [dsi.dsi_kv_length(c.kv, w) for w in range(4)] == lens
+
+
+def test_replayed_attention(dev):
+    """A captured step follows the lengths, what is still shared, and new inputs on every replay."""
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), Cache(8, 2, 128, "bf16", 3, 900) as c:
+        lens = forked(c, 0, range(3), 400, [0, 7, 20])
+        buf = c.rows(3 * 2)
+        out = c.attend(0, 3, 2, *buf)           # allocates
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            dsi.dsi_attend(c.model, c.kv, 0, 0, 3, 2, *buf, out, True)
+        for i in range(5):
+            if i == 2:
+                dsi.dsi_kv_rollback(c.kv, 1, 256)
+                c.fill(1, 256, 300)
+                dsi.dsi_kv_set_length(c.kv, 1, 300)
+                lens[1] = 300
+            if i == 4:                           # another root: what the graph was captured for is no longer shared
+                dsi.dsi_kv_set_length(c.kv, 2, lens[2])
+                dsi.dsi_kv_fork(c.kv, 2, 0, 2, 390)
+                lens[0] = lens[1] = 390
+            new = c.rows(3 * 2)
+            for x, y in zip(buf, new):
+                x.copy_(y)
+            out.fill_(7.0)
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            check(c, out, 0, 2, lens, *new)
+            lens = [n + 2 for n in lens]
+
+
+@pytest.mark.parametrize("name", ["tiny", "gqa_hd64"])
+def test_scored_continuations(dev, name, monkeypatch):
+    """Fork, verification and log probabilities together, against the oracle's decoder."""
+    from oracle import forward64
+    from paper_2405_14105_amd.executor import score_continuations
+
+    monkeypatch.setenv("DSI_SHARE", "1")
+    shape, T = S.SHAPES[name], 0.7
+    rng = np.random.default_rng(3)
+    prompt = rng.integers(0, shape.vocab, 200)
+    conts = [list(map(int, rng.integers(0, shape.vocab, n))) for n in (5, 3, 0, 4)]
+    get = lambda l, n: S.weight(shape, 0, l, n).astype(np.float64)
+    with Rig(shape, 0, 6, 240) as rig:
+        rig.prefill(5, prompt[:-1])
+        got = [score_continuations(rig.model, rig.kv, 5, 1, int(prompt[-1]), conts, shape.vocab, T, 3) for _ in range(2)]
+        assert [rig.length(w) for w in range(6)] == [0, 199, 199, 199, 199, 199]
+    assert got[0] == got[1]
+    # the project's bound on logits, for the token's and for log sum exp, over T; and fp32's rounding
+    tol = 2 * (1e-4 if shape.wdtype == "f32" else 2e-2) / T + 1e-5
+    for c, lp, H, ids, top in zip(conts, got[0].logprob, got[0].entropy, got[0].top_ids, got[0].top_logprobs):
+        assert len(lp) == len(H) == len(ids) == len(top) == len(c)
+        if not c:
+            continue
+        z = forward64(shape, get, np.concatenate([prompt, c[:-1]]))[0][len(prompt) - 1:] / T
+        ref = z - z.max(-1, keepdims=True)
+        ref -= np.log(np.exp(ref).sum(-1, keepdims=True))
+        for i, tok in enumerate(c):
+            assert abs(lp[i] - ref[i, tok]) <= tol
+            for j in range(3):
+                assert abs(top[i][j] - ref[i, ids[i][j]]) <= tol
+            assert abs(top[i][0] - ref[i].max()) <= tol
+            # entropy moves by at most tol (1 + |log p| spread) of the weights' change
+            assert abs(H[i] + (np.exp(ref[i]) * ref[i]).sum()) <= tol * (2 + np.abs(ref[i] * np.exp(ref[i])).sum())
+    with pytest.raises(ValueError):
+        score_continuations(0, 0, 0, 1, 0, [[1] * 40] * 2, shape.vocab)

@@ -100,6 +100,8 @@ def test_attend_refusals(stub):
 def test_what_runs_and_what_is_allocated(stub):
     """Windows that were not forked run as before; a step's buffers are allocated by its first call."""
     run(stub, '''
+    import os
+    os.environ["DSI_SHARE"] = "1"
     m = model(S.SHAPES["tiny"])
     kv = dsi.dsi_kv_create(m, 8, 2000)
     for w in range(8):
@@ -123,6 +125,16 @@ def test_what_runs_and_what_is_allocated(stub):
     # a chain of forks: the later root goes with its own
     dsi.dsi_kv_fork(kv, 4, 5, 1)
     assert "k_share" in verify(4, 2)
+    # what is known to share nothing worth it runs as before
+    dsi.dsi_kv_rollback(kv, 3, 127)
+    assert "k_attn" in verify(2, 2) and "k_share" in verify(4, 2)
+    dsi.dsi_kv_set_length(kv, 2, 100)
+    for w0, n in ((2, 3), (3, 2), (2, 2)):
+        assert "k_attn" in verify(w0, n) and "k_share" not in verify(w0, n)
+    dsi.dsi_kv_import(kv, 4, 0, 10, P, P)
+    assert "k_attn" in verify(0, 8) and "k_share" not in verify(0, 8)
+    dsi.dsi_kv_fork(kv, 6, 2, 4, 128)
+    assert "k_share" in verify(0, 8)
     attend = lambda rows, n=8: names(lambda: dsi.dsi_attend(m, kv, 0, 0, n, rows, P, P, P, P))
     assert attend(20) == {"k_share", "k_share_last"}
     for rows in (20, 1, 7):
@@ -134,6 +146,30 @@ def test_what_runs_and_what_is_allocated(stub):
     dsi.dsi_kv_fork(kv, 0, 1, 2, 64)
     hip.stub_capture(0)
     assert hip.stub_refused() == 0 and hip.stub_mallocs() == 0
+    ''')
+
+
+def test_a_prefix_is_read_once_where_that_saves_enough(stub):
+    run(stub, '''
+    import os
+    def kernels(m, kv, n):
+        dsi.dsi_profile_begin(m, dsi.DSI_K_ATTN)
+        hip.stub_clear()
+        dsi.dsi_verify(m, kv, 0, n, 1, P, P, P, P, P, commit=False)
+        return {k for k, _, _ in launches()}
+    each = 2 * 4 * 32 * 4                              # bytes of a position of a layer
+    for env in (None, "0", "1"):
+        os.environ.pop("DSI_SHARE", None)
+        if env:
+            os.environ["DSI_SHARE"] = env
+        m = model(S.SHAPES["tiny"])
+        kv = dsi.dsi_kv_create(m, 6, 20000)
+        for length in (100, 128, 13106, 13108, 19000):
+            dsi.dsi_kv_set_length(kv, 0, length)
+            dsi.dsi_kv_fork(kv, 0, 1, 5)
+            want = length >= 128 and env != "0" and (env == "1" or 5 * length * each >= 64 << 20)
+            assert ("k_share" in kernels(m, kv, 6)) == want, (env, length)
+            assert "k_share" not in kernels(m, kv, 1)
     ''')
 
 
