@@ -1,6 +1,7 @@
 // Host runtime behind the C ABI: model and KV-cache objects, the launch plan
 // of one target forward over a batch of window rows, and the verification /
 // prefill / rollback entry points.
+#include <limits.h>
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -1511,9 +1512,19 @@ dsi_status dsi_model_set_tensor(dsi_model* m, int32_t layer, int32_t id, const v
   return DSI_OK;
 }
 
+// bytes of the keys (and of the values) of such a cache
+static dsi_status kv_size(const dsi_model* m, int n_windows, int max_len, size_t* bytes) {
+  if (n_windows < 1 || max_len < 1) return fail(DSI_EINVAL, "n_windows and max_len must be >= 1");
+  if (max_len > INT_MAX - 63) return fail(DSI_EINVAL, "max_len must be at most %d", INT_MAX - 63);
+  // a position of a head in every layer and window stays below 2^63 bytes
+  const size_t pad = round_up((size_t)max_len, 64), rest = (size_t)m->hkv * m->hd * m->kvesz;
+  if (__builtin_mul_overflow((size_t)m->L * n_windows, pad, bytes) || __builtin_mul_overflow(*bytes, rest, bytes))
+    return fail(DSI_ENOMEM, "a cache of %d windows of %d positions", n_windows, max_len);
+  return DSI_OK;
+}
+
 // a cache object whose keys and values are still to come
 static dsi_status kv_new(dsi_model* m, int n_windows, int max_len, dsi_kv** out) {
-  if (n_windows < 1 || max_len < 1) return fail(DSI_EINVAL, "n_windows and max_len must be >= 1");
   dsi_kv* kv = new (std::nothrow) dsi_kv();
   if (!kv) return fail(DSI_ENOMEM, "host allocation failed");
   kv->m = m;
@@ -1521,22 +1532,25 @@ static dsi_status kv_new(dsi_model* m, int n_windows, int max_len, dsi_kv** out)
   kv->max_len = max_len;
   kv->maxlen_pad = (int)round_up((size_t)max_len, 64);
   kv->win_elems = (size_t)m->hkv * kv->maxlen_pad * m->hd;
-  kv->hi.assign(n_windows, 0);
-  kv->lo.assign(n_windows, 0);
-  kv->root.assign(n_windows, -1);
-  kv->shared.assign(n_windows, 0);
+  try {
+    kv->hi.assign(n_windows, 0);
+    kv->lo.assign(n_windows, 0);
+    kv->root.assign(n_windows, -1);
+    kv->shared.assign(n_windows, 0);
+  } catch (const std::bad_alloc&) {
+    delete kv;
+    return fail(DSI_ENOMEM, "host allocation failed");
+  }
   *out = kv;
   return DSI_OK;
-}
-static size_t kv_bytes(const dsi_kv* kv) {
-  return (size_t)kv->m->L * kv->n_windows * kv->win_elems * kv->m->kvesz;
 }
 
 dsi_status dsi_kv_create(dsi_model* m, int32_t n_windows, int32_t max_len, dsi_kv** out) {
   if (!m || !out) return fail(DSI_EINVAL, "null argument");
+  size_t bytes = 0;
+  DSI_TRY(kv_size(m, n_windows, max_len, &bytes));
   dsi_kv* kv = nullptr;
   DSI_TRY(kv_new(m, n_windows, max_len, &kv));
-  const size_t bytes = kv_bytes(kv);
   std::vector<void*> list;
   auto alloc = [&]() {
     dsi_status st = dev_alloc(list, &kv->k, bytes);
@@ -1558,10 +1572,9 @@ dsi_status dsi_kv_create(dsi_model* m, int32_t n_windows, int32_t max_len, dsi_k
 
 dsi_status dsi_kv_bytes(dsi_model* m, int32_t n_windows, int32_t max_len, size_t* bytes) {
   if (!m || !bytes) return fail(DSI_EINVAL, "null argument");
-  dsi_kv* kv = nullptr;
-  DSI_TRY(kv_new(m, n_windows, max_len, &kv));
-  *bytes = kv_bytes(kv);
-  delete kv;
+  size_t n = 0;
+  DSI_TRY(kv_size(m, n_windows, max_len, &n));
+  *bytes = n;
   return DSI_OK;
 }
 
@@ -1569,13 +1582,11 @@ dsi_status dsi_kv_wrap(dsi_model* m, int32_t n_windows, int32_t max_len, void* d
                        dsi_kv** out) {
   if (!m || !out || !d_k || !d_v) return fail(DSI_EINVAL, "null argument");
   if (((uintptr_t)d_k | (uintptr_t)d_v) & 15) return fail(DSI_EINVAL, "cache memory not 16-byte aligned");
+  size_t want = 0;
+  DSI_TRY(kv_size(m, n_windows, max_len, &want));
+  if (nbytes != want) return fail(DSI_EINVAL, "keys and values of this cache are %zu bytes each, got %zu", want, nbytes);
   dsi_kv* kv = nullptr;
   DSI_TRY(kv_new(m, n_windows, max_len, &kv));
-  if (nbytes != kv_bytes(kv)) {
-    const size_t want = kv_bytes(kv);
-    delete kv;
-    return fail(DSI_EINVAL, "keys and values of this cache are %zu bytes each, got %zu", want, nbytes);
-  }
   kv->owned = false;
   kv->k = d_k;
   kv->v = d_v;

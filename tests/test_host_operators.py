@@ -53,6 +53,15 @@ def test_wrap_refusals_and_ownership(stub):
             assert False, a
         except dsi.DsiError as e:
             assert e.status == dsi.DSI_EINVAL, a
+    # sizes that no memory holds are refused, not thrown or wrapped round
+    big = 2 ** 31 - 1
+    for f in (lambda w, l: dsi.dsi_kv_bytes(m, w, l), lambda w, l: dsi.dsi_kv_wrap(m, w, l, P, P, n), lambda w, l: dsi.dsi_kv_create(m, w, l)):
+        for w, l in ((big, big), (big, big - 63), (1, big), (big, 1 << 30)):
+            try:
+                f(w, l)
+                assert False
+            except dsi.DsiError as e:
+                assert e.status in (dsi.DSI_EINVAL, dsi.DSI_ENOMEM), e
     used = hip.stub_in_use()
     kv = dsi.dsi_kv_wrap(m, 3, 100, P, P, n)
     try:
