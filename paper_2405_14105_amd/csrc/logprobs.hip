@@ -36,6 +36,7 @@ constexpr int LPE = 16;                // entries per lane and step
 constexpr int LPS = 64 * LPE;          // entries per step
 constexpr int LPG = 4;                 // runs per lane of the join
 constexpr int kLpRuns = 64 * LPG;      // runs per row at most
+constexpr int kLpWaves = 3 * 1024;     // waves of a call: three a SIMD
 // up to so many alternatives are taken one by one (42 x 128256: 2 of them 18.7 us,
 // 4 21.9; 5 gathered 22.1)
 constexpr int kLpFew = 4;
@@ -380,7 +381,7 @@ __global__ __launch_bounds__(64) void k_lp_join(LogprobArgs a) {
 // 23.4, 34.1, 180.
 int lp_runs(long long rows, int V) {
   const long long steps = ((long long)V + LPS - 1) / LPS;
-  long long u = (3072 + rows - 1) / rows;
+  long long u = (kLpWaves + rows - 1) / rows;
   u = u < steps ? u : steps;
   return (int)(u < 1 ? 1 : u < kLpRuns ? u : kLpRuns);
 }

@@ -656,15 +656,15 @@ struct SharePlan {
 // 8192, 50 MB, 22.7 and 26.9; 32768 71 and 40)
 constexpr size_t kShareSaves = (size_t)64 << 20;
 
-// The host knows which window each was forked from; how much of it is still
-// shared is known on the device when the attention runs, so the partition goes
-// by the cache's capacity.
 // a window's rows from len on may change from now on (fork_cut, on the device)
 void cut_shared(dsi_kv* kv, int window, long long len) {
   for (int w = 0; w < kv->n_windows; ++w)
     if (w == window || kv->root[w] == window) kv->shared[w] = std::min(kv->shared[w], len);
 }
 
+// The host knows which window each was forked from; how much of it is still
+// shared is known on the device when the attention runs, so the partition goes
+// by the cache's capacity.
 SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, int R) {
   SharePlan p;
   ShareArgs& a = p.a;

@@ -33,9 +33,10 @@ __device__ __forceinline__ int wave_min(int v) {
 }
 
 // positions of the prefix that the group's windows share, whole blocks of 32
-// (each wave finds it for itself)
+// (each wave finds it for itself); never so many that the rows would not fit
+// behind them, whatever a length says
 __device__ __forceinline__ int group_prefix(const ShareArgs& a, const ShareGroup& g) {
-  int s = a.maxlen;
+  int s = a.maxlen - a.R;
   for (int i = threadIdx.x & 63; i < g.count; i += 64) {
     const int w = a.window0 + g.first + i;
     int x = a.f.lens[w];
@@ -78,11 +79,11 @@ struct KeyRange {
   int win, k0, k1, own;
 };
 
-// One part on the direct path: 16 queries, eight waves that take every eighth
-// 32-key step, keys and values straight from the cache into fragments (as in
-// the window attention: 16x16 MFMAs, S^T = K Q^T and O^T += V^T P^T, queries
-// and probabilities of a bf16 cache as hi + lo).  The waves' sums are joined in
-// LDS, where they lie as wave_sums.
+// One part on the direct path: 16 queries, NW waves that take every NW-th 32-key
+// step, keys and values straight from the cache into fragments (as in the window
+// attention: 16x16 MFMAs, S^T = K Q^T and O^T += V^T P^T, queries and
+// probabilities of a bf16 cache as hi + lo).  The waves' sums are left in LDS
+// (WaveSums) to be joined.
 // LAST: the second launch's part, with the rows of the call.  Values are summed
 // for VD of the head's dims, from d0 on.
 template <int NW, int VD>
