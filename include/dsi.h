@@ -290,9 +290,10 @@ dsi_status dsi_kv_wrap(dsi_model* m, int32_t n_windows, int32_t max_len, void* d
  * and length len; len = -1: all that src holds when the copy runs.  A prompt
  * then runs once, whatever the number of servers (Section 3.1, "KV cache")
  * that follow it.  What the windows held before is given up; their rows behind
- * len keep what they hold.  A len above src's length leaves them empty and is
- * reported by the next synchronising call (DSI_EINVAL).  Stream-ordered;
- * allocates nothing.
+ * len keep what they hold.  A len above src's length, or more positions than
+ * max_len (a replayed commit may have carried src's length past it), leaves
+ * them empty and is reported by the next synchronising call (DSI_EINVAL).
+ * Stream-ordered; allocates nothing.
  * The library remembers which positions a window still has in common with the
  * window it was forked from: they end where either is rolled back, forked into
  * or imported to.  dsi_verify, dsi_verify_tree and dsi_attend read the

@@ -423,6 +423,7 @@ struct ForkArgs {
   int n_layers, n_kv, hd, maxlen, esz;
   int src, window0, n;
   int len;              // positions taken, -1: the source's length
+  int most;             // positions of a window at most
   int* err;
 };
 hipError_t launch_kv_fork(const ForkArgs& a, int max_len, hipStream_t s);

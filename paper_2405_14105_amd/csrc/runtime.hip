@@ -1161,7 +1161,7 @@ dsi_status check_err_word(int* err, hipStream_t s) {
     if (h & 2) what += " verification input invalid (token id or q(d) <= 0);";
     if (h & 4) what += " rollback above the current length;";
     if (h & 8) what += " token-tree parent array invalid;";
-    if (h & 16) what += " fork beyond the source's length;";
+    if (h & 16) what += " fork beyond the source's length or the cache's;";
     return fail(DSI_EINVAL, "device-detected input error:%s", what.c_str());
   }
   return DSI_OK;
@@ -1959,6 +1959,7 @@ dsi_status dsi_kv_fork(dsi_kv* kv, int32_t src, int32_t window0, int32_t n_windo
   a.window0 = window0;
   a.n = n_windows;
   a.len = len;
+  a.most = kv->max_len;
   a.err = m->err;
   (void)capturing(kv->m);
   HIP_TRY(launch_kv_fork(a, len < 0 ? (int)kv->hi[src] : len, m->stream));

@@ -794,7 +794,8 @@ __global__ __launch_bounds__(256) void k_kv_fork(ForkArgs a) {
   const int have = a.f.lens[a.src];
   const int len = a.len < 0 ? have : a.len;
   const bool first = blockIdx.x == 0 && blockIdx.y == 0;
-  const bool bad = len > have;
+  // a replayed commit of the caller's may have carried a length past the cache's end
+  const bool bad = len > have || len > a.most;
   constexpr int VE = 16 / ESZ;           // elements per 16 bytes
   constexpr int MOST = 128 * 32 / VE / 256;   // 16-byte pieces per thread of a block's keys (and values)
   const int pieces = a.hd * 32 / VE;

@@ -285,6 +285,37 @@ def test_fork_beyond_the_source_is_reported(dev):
         assert [rig.length(w) for w in range(3)] == [60, 40, 40]
 
 
+def test_fork_of_a_window_past_the_caches_end(dev):
+    """Replayed commits carry a length past max_len (still within the cache's last
+    block of positions); a fork takes no positions from there and is reported."""
+    shape, side = S.SHAPES["tiny"], torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), Rig(shape, 0, 3, 100) as rig:
+        rig.prefill(0, np.arange(90))
+        rig.prefill(1, np.arange(9))
+        rig.prefill(2, np.arange(7))
+        t = rig.dev_i32([1])
+        step = lambda: dsi.dsi_prefill(rig.model, rig.kv, 0, t, 1, None)
+        step()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            step()
+        for _ in range(14):                      # 91 + 14 positions; the cache's memory holds 128
+            g.replay()
+        torch.cuda.synchronize()
+        dsi.dsi_kv_fork(rig.kv, 0, 1, 1)
+        with pytest.raises(dsi.DsiError, match="fork beyond"):
+            dsi.dsi_sync(rig.model)
+        assert [rig.length(w) for w in range(3)] == [105, 0, 7]
+        dsi.dsi_kv_rollback(rig.kv, 0, 100)
+        dsi.dsi_kv_fork(rig.kv, 0, 1, 2)
+        assert [rig.length(w) for w in range(3)] == [100, 100, 100]
+        for w in (1, 2):
+            for x, y in zip(rig.export_kv(0, 0, 100), rig.export_kv(w, 0, 100)):
+                assert np.array_equal(x, y)
+
+
 # ------------------------------------------------------------------- verification
 
 
