@@ -26,6 +26,12 @@
  *    q(d) not positive and finite, an invalid token-tree parent) make the affected window output
  *    n = -1, token = -1, leave its KV length unchanged, and make the next
  *    synchronising call (dsi_sync, dsi_kv_length) return DSI_EINVAL.
+ *  - Capacities (DSI_ECAPACITY) are checked against host bounds on the lengths,
+ *    which are on the device.  A call that the caller captures into a graph of
+ *    its own moves the bounds once, when it is captured, not when it is
+ *    replayed.  After replays of calls that commit, append or fork,
+ *    dsi_kv_length makes a window's bound its length; so does it before further
+ *    calls on that window, and the caller replays only what fits.
  *  - A dsi_model's weights are immutable after they are set and the model
  *    may serve several dsi_kv; calls on one model (and its KV caches) must
  *    not overlap: the model's forward workspaces are shared by all of them.
@@ -321,7 +327,9 @@ dsi_status dsi_kv_fork(dsi_kv* kv, int32_t src, int32_t window0, int32_t n_windo
  *   d_out          [n_windows*rows][n_heads][head_dim] fp32, 16-byte aligned
  * The model's weights are not used and need not be set.  Runs on the model's
  * stream; its first call of a size allocates (capture later ones).  Fails with
- * DSI_ECAPACITY if a length + rows may exceed max_len.
+ * DSI_ECAPACITY if a length + rows may exceed max_len.  A window whose rows no
+ * longer fit when a captured call is replayed gets NaN, keeps its cache and
+ * length, and is reported by the next synchronising call (DSI_EINVAL).
  * Numerics: fp32-accurate queries and probabilities against the cache's type,
  * fp32 sums.  A key or value of a row that is not finite reaches only the rows
  * that see it. */

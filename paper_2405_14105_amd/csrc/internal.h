@@ -445,6 +445,8 @@ struct ShareArgs {
   // cache yet: the launch puts them there
   const float* k_new;
   const float* v_new;
+  int* err;             // with k_new: told of windows whose rows do not fit max_len
+  int max_len;          // positions of a window; maxlen is rounded up
   ForkState f;
   int window0, B, R;
   int n_heads, n_kv, maxlen;
@@ -463,7 +465,7 @@ struct ShareArgs {
 };
 int share_tile(int kv_bf16, int queries);
 hipError_t launch_attention_shared(int kv_bf16, int hd, const ShareArgs& a, hipStream_t s);
-hipError_t launch_kv_advance(int* lens, int window0, int B, int rows, hipStream_t s);
+hipError_t launch_kv_advance(int* lens, int window0, int B, int rows, int max_len, hipStream_t s);
 
 // KV and misc (elementwise.hip)
 hipError_t launch_kv_rollback(const ForkState& f, int window, int new_len, int* err, hipStream_t s);

@@ -728,6 +728,7 @@ ShareArgs share_args(const dsi_model* m, const dsi_kv* kv, const SharePlan& p, i
   a.n_heads = m->hq;
   a.n_kv = m->hkv;
   a.maxlen = kv->maxlen_pad;
+  a.max_len = kv->max_len;
   a.scale = (float)(1.0 / sqrt((double)m->hd));
   a.part_o = m->attn_o;
   a.part_ml = m->attn_ml;
@@ -1162,6 +1163,7 @@ dsi_status check_err_word(int* err, hipStream_t s) {
     if (h & 4) what += " rollback above the current length;";
     if (h & 8) what += " token-tree parent array invalid;";
     if (h & 16) what += " fork beyond the source's length or the cache's;";
+    if (h & 32) what += " attention rows beyond the cache's end (a replayed call);";
     return fail(DSI_EINVAL, "device-detected input error:%s", what.c_str());
   }
   return DSI_OK;
@@ -1997,10 +1999,11 @@ dsi_status dsi_attend(dsi_model* m, dsi_kv* kv, const dsi_attend_args* a) {
   sa.out_rows = a->d_out;
   sa.k_new = a->d_k;
   sa.v_new = a->d_v;
+  sa.err = m->err;
   Prof p(m, DSI_K_ATTN);
   HIP_TRY(launch_attention_shared(m->kvb, m->hd, sa, m->stream));
   if (a->commit) {
-    HIP_TRY(launch_kv_advance(kv->lens, a->window0, B, R, m->stream));
+    HIP_TRY(launch_kv_advance(kv->lens, a->window0, B, R, kv->max_len, m->stream));
     for (int b = 0; b < B; ++b) kv->hi[a->window0 + b] += R;
   }
   return DSI_OK;

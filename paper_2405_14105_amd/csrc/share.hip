@@ -606,11 +606,16 @@ __device__ void tile_part(const ShareArgs& a, const QuerySet& qs, const ShareGro
 
 // the rows' keys and values of one window and KV head into the slots behind its
 // length, rounded to the cache's type: keys by dims, values by positions, so that
-// neighbouring threads write neighbours
+// neighbouring threads write neighbours.  The host has checked that they fit, but
+// for calls that the caller replays: there is nothing cached where they do not.
 template <int KVB, int HD>
 __device__ void append_rows(const ShareArgs& a, int win, int kvh) {
   const int len = a.f.lens[a.window0 + win];
-  const int n = min(a.R, a.maxlen - len);
+  const int n = a.R;
+  if (len > a.max_len - n) {
+    if (kvh == 0 && threadIdx.x == 0) atomicOr(a.err, 32);
+    return;
+  }
   const size_t base = ((size_t)(a.window0 + win) * a.n_kv + kvh) * (size_t)a.maxlen * HD;
   const size_t row = (size_t)a.n_kv * HD, from = (size_t)win * a.R * row + (size_t)kvh * HD;
   for (int i = threadIdx.x; i < n * HD; i += SW * 64) {
@@ -746,7 +751,8 @@ __global__ __launch_bounds__(LW * 64, KVB ? 2 : 1) void k_share_last(ShareArgs a
         acc += o[j] * f;
       }
   }
-  const float inv = 1.0f / L;
+  // a replayed call's rows that did not fit were not cached: no result
+  const float inv = a.k_new && a.f.lens[a.window0 + win] > a.max_len - a.R ? NAN : 1.0f / L;
   const float y4[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
   if (a.out_rows) *(float4*)(a.out_rows + r * HD + d) = float4{y4[0], y4[1], y4[2], y4[3]};
   else pack_store4(a.out, a.wtype, m, head * HD + d, y4);
@@ -775,8 +781,9 @@ hipError_t launch_shared_hd(int kv_bf16, const ShareArgs& a, hipStream_t s) {
   return hipErrorInvalidValue;
 }
 
-__global__ void k_kv_advance(int* lens, int window0, int B, int rows) {
-  for (int b = threadIdx.x; b < B; b += blockDim.x) lens[window0 + b] += rows;
+__global__ void k_kv_advance(int* lens, int window0, int B, int rows, int max_len) {
+  for (int b = threadIdx.x; b < B; b += blockDim.x)
+    if (lens[window0 + b] <= max_len - rows) lens[window0 + b] += rows;
 }
 
 __global__ void k_fork_cut(ForkState f, int window, int new_len) { fork_cut(f, window, new_len); }
@@ -871,8 +878,8 @@ hipError_t launch_attention_shared(int kv_bf16, int hd, const ShareArgs& a, hipS
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_kv_advance(int* lens, int window0, int B, int rows, hipStream_t s) {
-  hipLaunchKernelGGL(k_kv_advance, dim3(1), dim3(64), 0, s, lens, window0, B, rows);
+hipError_t launch_kv_advance(int* lens, int window0, int B, int rows, int max_len, hipStream_t s) {
+  hipLaunchKernelGGL(k_kv_advance, dim3(1), dim3(64), 0, s, lens, window0, B, rows, max_len);
   return hipGetLastError();
 }
 

@@ -457,6 +457,54 @@ def test_replayed_attention(dev):
             lens = [n + 2 for n in lens]
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_replays_until_the_cache_is_full(dev, kind):
+    """A captured step replayed past max_len is reported: the full window gets no
+    result and keeps its cache, the others go on."""
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), Cache(4, 2, 64, kind, 4, 200) as c:
+        lens = forked(c, 0, range(4), 130, [0, 62, 5, 63])
+        buf = c.rows(3 * 3)
+        out = c.attend(0, 3, 3, *buf)            # allocates
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            dsi.dsi_attend(c.model, c.kv, 0, 0, 3, 3, *buf, out, True)
+        for i in range(5):
+            new = c.rows(3 * 3)
+            for x, y in zip(buf, new):
+                x.copy_(y)
+            out.fill_(7.0)
+            before = c.k.clone(), c.v.clone()
+            g.replay()
+            torch.cuda.synchronize()
+            full = lens[1] + 3 > 200
+            assert full == (i >= 2)
+            for b in range(3):
+                sl = slice(3 * b, 3 * b + 3)
+                if b == 1 and full:
+                    assert out[sl].isnan().all()
+                else:
+                    ref, tol = attention64(c, b, lens[b], *(x[sl] for x in new))
+                    assert ((out[sl].double() - ref).abs() <= tol).all(), (i, b)
+                    lens[b] += 3
+            word = torch.int16 if kind == "bf16" else torch.int32
+            for now, was in zip((c.k, c.v), before):   # the full window, and the one behind the call
+                assert torch.equal(now[:, 3].view(word), was[:, 3].view(word))
+                assert not full or torch.equal(now[:, 1].view(word), was[:, 1].view(word))
+            if full:
+                with pytest.raises(dsi.DsiError, match="beyond the cache's end"):
+                    dsi.dsi_sync(c.model)
+            else:
+                dsi.dsi_sync(c.model)
+        assert [dsi.dsi_kv_length(c.kv, w) for w in range(4)] == lens == [145, 198, 150, 193]
+        dsi.dsi_kv_fork(c.kv, 1, 0, 1)
+        q, k, v = c.rows(2)
+        assert dsi.dsi_kv_length(c.kv, 0) == 198
+        check(c, c.attend(0, 1, 2, q, k, v), 0, 2, [198], q, k, v)
+
+
 @pytest.mark.parametrize("name", ["tiny", "gqa_hd64"])
 def test_scored_continuations(dev, name, monkeypatch):
     """Fork, verification and log probabilities together, against the oracle's decoder."""
