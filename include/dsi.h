@@ -326,7 +326,8 @@ dsi_status dsi_kv_fork(dsi_kv* kv, int32_t src, int32_t window0, int32_t n_windo
  *                  not committed)
  *   d_out          [n_windows*rows][n_heads][head_dim] fp32, 16-byte aligned
  * The model's weights are not used and need not be set.  Runs on the model's
- * stream; its first call of a size allocates (capture later ones).  Fails with
+ * stream; its first call of a size (windows, rows, cache) allocates what calls of
+ * that size need whatever is forked then: capture later ones.  Fails with
  * DSI_ECAPACITY if a length + rows may exceed max_len.  A window whose rows no
  * longer fit when a captured call is replayed gets NaN, keeps its cache and
  * length, and is reported by the next synchronising call (DSI_EINVAL).

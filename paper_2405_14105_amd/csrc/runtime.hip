@@ -155,6 +155,7 @@ struct dsi_model {
   // partials of chunked attention, attn_parts (row, chunk) rows of them, in one
   // allocation, and the outgrown ones (ensure_attention)
   size_t attn_parts = 0;
+  size_t attn_refused = SIZE_MAX;  // partial rows there was no memory for (dsi_attend)
   float* attn_o = nullptr;
   float2* attn_ml = nullptr;
   void* attn_slab[64] = {};
@@ -712,6 +713,15 @@ SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, 
   }
   p.parts = (size_t)(a.p_chunks + a.t_chunks) * B * R * m->hq;
   return p;
+}
+
+// Partial rows that B windows of R rows need at most, however they are forked:
+// one group, of two windows, makes the most chunks of a prefix.
+size_t share_parts(const dsi_model* m, const dsi_kv* kv, int B, int R) {
+  const int queries = m->hq / m->hkv * R, tile = m->kvb ? 256 : 16;
+  const int own = std::max(1, 512 / (B * m->hkv * cdiv(queries, 16)));
+  const int prefix = B > 1 ? std::max(1, 256 / (m->hkv * cdiv(2 * queries, tile))) : 0;
+  return (size_t)(std::min(prefix, cdiv(kv->max_len, 128)) + std::min(own, cdiv(kv->max_len, 256))) * B * R * m->hq;
 }
 
 // whether a forward takes the plan
@@ -1619,6 +1629,7 @@ dsi_status dsi_kv_destroy(dsi_kv* kv) {
   hipFree(kv->lens);
   kv->m->live_kv--;
   kv->m->wide_wait = 0;
+  kv->m->attn_refused = SIZE_MAX;
   delete kv;
   return DSI_OK;
 }
@@ -1988,12 +1999,17 @@ dsi_status dsi_attend(dsi_model* m, dsi_kv* kv, const dsi_attend_args* a) {
   if (!a->d_q || !a->d_k || !a->d_v || !a->d_out) return fail(DSI_EINVAL, "null queries, keys, values or output pointer");
   if (((uintptr_t)a->d_q | (uintptr_t)a->d_k | (uintptr_t)a->d_v | (uintptr_t)a->d_out) & 15)
     return fail(DSI_EINVAL, "queries, keys, values or output not 16-byte aligned");
-  (void)capturing(m);
+  const bool cap = capturing(m);
   for (int b = 0; b < B; ++b)
     if (kv->hi[a->window0 + b] + R > kv->max_len)
       return fail(DSI_ECAPACITY, "window %d: length (<= %lld) + %d exceeds max_len %d", a->window0 + b,
                   kv->hi[a->window0 + b], R, kv->max_len);
   const SharePlan sp = plan_shared(m, kv, a->window0, B, R);
+  // what the size needs, whatever is forked when a later call is captured; where
+  // there is no memory for that (until a cache has been destroyed), what this call
+  // needs
+  const size_t most = share_parts(m, kv, B, R);
+  if (!cap && most < m->attn_refused && ensure_attention(m, most) != DSI_OK) m->attn_refused = most;
   DSI_TRY(ensure_attention(m, sp.parts));
   ShareArgs sa = share_args(m, kv, sp, a->layer, a->d_q);
   sa.out_rows = a->d_out;

@@ -158,6 +158,50 @@ def test_what_runs_and_what_is_allocated(stub):
     ''')
 
 
+def test_the_first_call_of_a_size_allocates_for_any_forks(stub):
+    """A step captured after windows were forked or rolled back finds its buffers, whatever was forked at its first call."""
+    run(stub, '''
+    import random
+    rng = random.Random(1)
+    for hq, hkv, hd, kind, W, max_len in ((32, 8, 128, dsi.DSI_BF16, 4, 32768), (8, 8, 64, dsi.DSI_BF16, 6, 3000), (32, 8, 64, dsi.DSI_F32, 5, 9000),
+                                          (40, 40, 128, dsi.DSI_BF16, 8, 8192), (4, 1, 32, dsi.DSI_F32, 12, 700), (64, 8, 128, dsi.DSI_BF16, 16, 4096)):
+        for rows in (1, 6, 17, 64):
+            m = dsi.dsi_model_create(dsi.make_config(1, 32, hq, hkv, hd, 32, 32, kvdtype=kind), STREAM)
+            kv = dsi.dsi_kv_create(m, W, max_len)
+            attend = lambda w0, n: dsi.dsi_attend(m, kv, 0, w0, n, rows, P, P, P, P)
+            for w in range(W):
+                dsi.dsi_kv_set_length(kv, w, max_len - rows)
+            for n in range(1, W + 1):
+                attend(0, n)
+            for turn in range(30):
+                for _ in range(rng.randint(1, 4)):
+                    src, w0 = rng.randrange(W), rng.randrange(W)
+                    n = rng.randint(1, W - w0)
+                    if src < w0 or src >= w0 + n:
+                        dsi.dsi_kv_fork(kv, src, w0, n)
+                    if rng.random() < 0.3:
+                        dsi.dsi_kv_set_length(kv, rng.randrange(W), rng.choice((0, 100, 500, max_len - rows)))
+                hip.stub_clear()
+                hip.stub_capture(1)
+                w0 = rng.randrange(W)
+                attend(w0, rng.randint(1, W - w0))
+                attend(0, W)
+                hip.stub_capture(0)
+                assert hip.stub_refused() == 0 and hip.stub_mallocs() == 0, (hq, hkv, hd, rows, turn)
+            dsi.dsi_kv_destroy(kv)
+            dsi.dsi_model_destroy(m)
+    # where there is no room for all that, a call takes what it needs itself
+    m = dsi.dsi_model_create(dsi.make_config(1, 32, 32, 8, 128, 32, 32, kvdtype=dsi.DSI_BF16), STREAM)
+    kv = dsi.dsi_kv_create(m, 4, 32768)
+    hip.stub_budget(17 * 4 * 32 * (128 * 4 + 8) + 8192)
+    for _ in range(3):
+        dsi.dsi_attend(m, kv, 0, 0, 4, 1, P, P, P, P)
+    hip.stub_clear()
+    dsi.dsi_attend(m, kv, 0, 0, 4, 1, P, P, P, P)
+    assert hip.stub_refused() == 0                       # not asked for again and again
+    ''')
+
+
 def test_a_prefix_is_read_once_where_that_saves_enough(stub):
     run(stub, '''
     import os
