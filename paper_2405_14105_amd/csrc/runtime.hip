@@ -724,9 +724,12 @@ size_t share_parts(const dsi_model* m, const dsi_kv* kv, int B, int R) {
   return (size_t)(std::min(prefix, cdiv(kv->max_len, 128)) + std::min(own, cdiv(kv->max_len, 256))) * B * R * m->hq;
 }
 
-// whether a forward takes the plan
-bool share_forward(const dsi_model* m, const SharePlan& p) {
-  return p.a.n_groups > 0 && (m->share == 1 || (m->share < 0 && p.saved >= kShareSaves));
+// Whether a forward takes the plan, whose partials are then allocated.  Where
+// that is not possible (a captured call, no memory) the window kernels run, whose
+// buffers it has.
+bool share_forward(dsi_model* m, const SharePlan& p) {
+  if (!p.a.n_groups || m->share == 0 || (m->share < 0 && p.saved < kShareSaves)) return false;
+  return p.parts <= m->attn_parts || (!capturing(m) && ensure_attention(m, p.parts) == DSI_OK);
 }
 
 ShareArgs share_args(const dsi_model* m, const dsi_kv* kv, const SharePlan& p, int layer, const float* q) {
@@ -1685,7 +1688,6 @@ dsi_status dsi_verify(dsi_model* m, dsi_kv* kv, const dsi_verify_args* a, int32_
   DSI_TRY(plan_attention(m, kv, a->window0, B, k + 1, &ap));
   const SharePlan sp = plan_shared(m, kv, a->window0, B, k + 1);
   const bool share = share_forward(m, sp);
-  if (share) DSI_TRY(ensure_attention(m, sp.parts));
   m->last_window0 = a->window0;
   m->last_B = B;
   m->last_R = k + 1;
@@ -1760,7 +1762,6 @@ dsi_status dsi_verify_tree(dsi_model* m, dsi_kv* kv, const dsi_tree_args* a, int
   DSI_TRY(plan_attention(m, kv, a->window0, B, R, &ap));
   const SharePlan sp = plan_shared(m, kv, a->window0, B, R);
   const bool share = share_forward(m, sp);
-  if (share) DSI_TRY(ensure_attention(m, sp.parts));
   m->last_window0 = a->window0;
   m->last_B = B;
   m->last_R = R;

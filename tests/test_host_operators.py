@@ -202,6 +202,44 @@ def test_the_first_call_of_a_size_allocates_for_any_forks(stub):
     ''')
 
 
+def test_forwards_without_room_for_a_shared_prefix_run_as_before(stub):
+    """Captured after windows were forked, or short of memory: the window kernels, no refusal."""
+    run(stub, '''
+    import os
+    os.environ["DSI_SHARE"], os.environ["DSI_GRAPHS"] = "1", "0"
+    def names(f):
+        hip.stub_clear()
+        f()
+        return {k for k, _, _ in launches()}
+    for how in ("capture", "memory"):
+        m = model(S.SHAPES["gqa_hd64"])
+        kv = dsi.dsi_kv_create(m, 4, 900)
+        verify = lambda: dsi.dsi_verify(m, kv, 0, 4, 5, P, P, P, P, P, commit=False)
+        tree = lambda: dsi.dsi_verify_tree(m, kv, 0, 4, 6, P, P, P, P, P, commit=False)
+        for w in range(4):
+            dsi.dsi_prefill(m, kv, w, P, 600, P)
+        for f in (verify, tree):
+            assert "k_attn" in names(f)
+        dsi.dsi_kv_fork(kv, 0, 1, 3)
+        for f in (verify, tree):
+            if how == "capture":
+                hip.stub_capture(1)
+            else:
+                hip.stub_budget(0)
+            got = names(f)
+            assert "k_attn" in got and "k_share" not in got
+            hip.stub_capture(0)
+            hip.stub_budget(1 << 40)
+        for f in (verify, tree):                         # with room, and captured once there is some
+            assert "k_share" in names(f)
+            hip.stub_capture(1)
+            assert "k_share" in names(f) and hip.stub_refused() == 0
+            hip.stub_capture(0)
+        dsi.dsi_kv_destroy(kv)
+        dsi.dsi_model_destroy(m)
+    ''')
+
+
 def test_a_prefix_is_read_once_where_that_saves_enough(stub):
     run(stub, '''
     import os
