@@ -8,8 +8,9 @@
 // lane and step, the next step's loads in flight while one is worked on.  A
 // lane keeps a running maximum, and sums relative to it that are rescaled when
 // it moves: the 16 terms of a step are added in fp32, the steps in fp64.  The
-// entries equal to the maximum are counted, not summed, so that S - 1 of a
-// row that is sure of one token keeps its digits (log1p).
+// entries equal to the maximum are counted, not summed: log S = log c + log1p(s / c)
+// of c such entries and the others' sum s keeps its digits where a row is sure of
+// one token.
 // Alternatives: a wave keeps its largest entries sorted across its lanes, key =
 // (logit in unsigned order, id complemented).  A step whose lanes hold nothing
 // above the n-th key costs one ballot.  Otherwise a few alternatives are taken
@@ -323,13 +324,15 @@ __global__ __launch_bounds__(64) void k_lp_join(LogprobArgs a) {
     M = fmaxf(M, x[j].m);
   }
   M = wave_max(M);
-  double s = 0.0, t = 0.0;
+  // c entries equal the row's maximum, the others' sum is s: S = c + s
+  double c = 0.0, s = 0.0, t = 0.0;
   const double ln2 = 0.69314718055994530942;
 #pragma unroll
   for (int j = 0; j < LPG; ++j) {
     const double all = x[j].rest + (double)x[j].cnt;
     if (x[j].m == M || x[j].m == -INFINITY) {
-      s += all;
+      c += (double)x[j].cnt;
+      s += x[j].rest;
       t += x[j].t * ln2;
     } else {
       const double d = ((double)x[j].m - (double)M) * a.inv_temperature, f = exp(d);
@@ -337,13 +340,14 @@ __global__ __launch_bounds__(64) void k_lp_join(LogprobArgs a) {
       t += f > 0.0 ? (x[j].t * ln2 + d * all) * f : 0.0;
     }
   }
+  c = wave_sum(c);
   s = wave_sum(s);
   t = wave_sum(t);
   // a row of -inf, and one with +inf, has no distribution
   const bool none = !isfinite(M);
-  const double lse = none ? (double)NAN : log1p(s - 1.0);
+  const double lse = none ? (double)NAN : log(c) + log1p(s / c);
   if (lane == 0) {
-    if (a.entropy) a.entropy[r] = (float)(lse - t / s);
+    if (a.entropy) a.entropy[r] = (float)(lse - t / (c + s));
     if (a.logprob) {
       const int tok = a.tokens[r];
       float lp = NAN;

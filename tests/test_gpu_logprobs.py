@@ -164,6 +164,30 @@ def test_a_sure_row_keeps_its_digits(dev):
     assert ((o["entropy"].double() - H).abs() <= H * 2.0 ** -16 + 2.0 ** -45).all()
 
 
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [2, 1000, 40000])
+@pytest.mark.parametrize("margin", [17.0, 25.0, 40.0, 60.0, 80.0])
+def test_a_sure_row_is_exact_relative_to_itself(dev, dt, V, margin):
+    """1 - p far below the step of 1 in any type: log p, the entropy and the
+    alternatives keep their digits, whichever run holds the token."""
+    at = sorted({0, V // 3, V - 1})
+    z = torch.full((len(at), V), 3.0, device="cuda", dtype=dt)
+    for r, i in enumerate(at):
+        z[r, i] = 3.0 + margin
+    t = torch.tensor(at, device="cuda", dtype=torch.int32)
+    o = call(z, t, 2)
+    rest = (V - 1) * math.exp(-margin)
+    lp, H = -math.log1p(rest), math.log1p(rest) + rest / (1 + rest) * margin
+    # each e^-margin: its exponent's factor and product, 2^-24 of the exponent each,
+    # exp2's ulp, and the sums of 16 terms (16 2^-24); the mean of the exponents has
+    # those once more, the result its rounding
+    tol = margin * 2.0 ** -23 + 2.0 ** -19
+    assert ((o["logprob"].double() - lp).abs() <= -lp * tol).all()
+    assert ((o["top"][:, 0].double() - lp).abs() <= -lp * tol).all()
+    assert ((o["entropy"].double() - H).abs() <= H * 2 * tol).all()
+    assert o["ids"][:, 0].tolist() == at and o["ids"][:, 1].tolist() == [1 if i == 0 else 0 for i in at]
+
+
 def test_targets_outside_the_vocabulary(dev):
     z, _ = logits(4, 900, 5)
     t = torch.tensor([-1, 900, 2 ** 30, 899], device="cuda", dtype=torch.int32)
