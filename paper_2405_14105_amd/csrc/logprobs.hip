@@ -115,6 +115,13 @@ __device__ __forceinline__ void merge_keys(u64& list, u64 keys, int lane) {
   list = list > keys ? list : keys;   // the larger ones, as a bitonic sequence
   sort_steps<64, 32, true>(list, lane);
 }
+// what the wave's lanes wrote to LDS is there for all of them: the LDS takes a
+// wave's accesses in their order, the compiler is told to keep it
+__device__ __forceinline__ void lanes_see() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 // the lane above takes this lane's value (wave_shr:1); lane 0 keeps its own
 __device__ __forceinline__ u64 from_lane_below(u64 v) {
   const int hi = __builtin_amdgcn_update_dpp((int)(v >> 32), (int)(v >> 32), 0x138, 0xF, 0xF, false);
@@ -281,15 +288,19 @@ __global__ __launch_bounds__(LPW * 64) void k_lp_rows(LogprobArgs a) {
           }
           have += __popcll(mask);
           if (have >= 64) {
+            lanes_see();
             merge_keys(list, held[lane], lane);
             have -= 64;
             if (lane < have) held[lane] = held[64 + lane];
+            lanes_see();
             tau = (uint32_t)(lane_key(list, a.n - 1) >> 32);
             bar = bar > tau ? bar : tau;
           }
         }
         if (have) {
+          lanes_see();
           merge_keys(list, lane < have ? held[lane] : 0, lane);
+          lanes_see();
           tau = (uint32_t)(lane_key(list, a.n - 1) >> 32);
         }
       }
