@@ -433,6 +433,7 @@ hipError_t launch_fork_cut(const ForkState& f, int window, int new_len, hipStrea
 // share read once for all of them (share.hip).
 constexpr int kMaxForkGroups = kMaxRows / 2;
 constexpr int kMinShared = 128;   // a shorter shared prefix is read by each window
+constexpr int kShareLast = 256;   // cached keys of a window's own that the second launch takes at most
 struct ShareGroup {
   int first, count;     // windows of the call
   int root;             // the window forked from

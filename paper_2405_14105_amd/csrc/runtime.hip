@@ -646,9 +646,13 @@ struct SharePlan {
   ShareArgs a{};        // groups, tiles and chunks; the rest by share_args
   size_t parts = 0;     // partial rows
   size_t saved = 0;     // bytes of keys and values that need not be read again
+  size_t own = 0;       // and of those that a window does not share
 };
 
-// A forward reads a shared prefix once where that saves so much in a layer; below,
+// A forward reads a shared prefix once where that saves so much in a layer, and a
+// quarter of what its windows have of their own, which the window kernels read
+// faster (13B, 8 x 1 rows, 86 MB saved: with 671 MB of their own 128 us by themselves,
+// 147 shared, with 246 MB 77 and 74); below,
 // the window kernels are faster, whose workgroups are smaller and more (us a
 // layer, by themselves and shared.  8B, 7 windows of 6 rows: 2048 positions, 50
 // MB, 28.1 and 28.7; 4096 46.7 and 33.8; 32768 219 and 79; 2 of 11: 8192, 34 MB,
@@ -678,20 +682,32 @@ SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, 
     return j - i;
   };
   int most = 0;
-  for (int i = 0; i < B && a.n_groups < kMaxForkGroups;) {
+  long long longest = 0, total = 0;   // keys of the windows' own that the first launch takes
+  const size_t each = 2 * (size_t)m->kvdim * m->kvesz;   // bytes of a position
+  for (int i = 0; i < B;) {
     const int w = window0 + i;
     int r = w, n = run(i, w);
     if (kv->root[w] >= 0 && run(i, kv->root[w]) > n) n = run(i, r = kv->root[w]);
+    if (a.n_groups == kMaxForkGroups) n = 1;
+    long long common = 0;
     if (n > 1) {
       a.group[a.n_groups++] = ShareGroup{i, n, r};
       most = std::max(most, n);
-      long long common = kv->max_len;
+      common = kv->max_len;
       for (int j = i; j < i + n; ++j)
         common = std::min(common, window0 + j == r ? kv->hi[r] : kv->shared[window0 + j]);
-      p.saved += (size_t)(n - 1) * common * 2 * m->kvdim * m->kvesz;
+      p.saved += (n - 1) * common * each;
+      common = common < kMinShared ? 0 : common / 32 * 32;
+    }
+    for (int j = i; j < i + n; ++j) {
+      const long long own = kv->hi[window0 + j] - common;
+      if (own <= kShareLast) continue;
+      longest = std::max(longest, own);
+      total += own;
     }
     i += n;
   }
+  p.own = (size_t)total * each;
   const int G = m->hq / m->hkv;
   a.p_tile = share_tile(m->kvb, G * R * most);
   // a short cache's prefix makes few parts: smaller tiles, whose keys are read
@@ -704,7 +720,25 @@ SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, 
   // forked ones have little of their own, and most of these workgroups only
   // cache the rows (6 x 7 rows over 1024 shared keys, 13B: 17.6 us with 480 of
   // them, 16.7 with 240)
-  a.t_chunks = std::min(std::max(1, (a.n_groups ? 128 : 512) / (B * m->hkv * a.t_tiles)), cdiv(kv->max_len, 256));
+  const int units = m->hkv * a.t_tiles;
+  a.t_chunks = std::max(1, (a.n_groups ? 128 : 512) / (B * units));
+  if (a.n_groups && longest) {
+    // Some have more, by what the host knows: chunks for one round of workgroups
+    // that have keys, or where one chunk makes more than a round, for rounds that
+    // are full; 1024 workgroups in all (us a layer with one chunk, these, and each
+    // window by itself.  8B, 7 x 6 rows over 5461 shared keys: 4096 of each one's own
+    // 79, 65, 77; a window beside them of 16384 that shares nothing 179, 63, 81; 2 x
+    // 11 over 32768, one of 32768 beside them 327, 114, 116.  13B, 8 x 1 over 2048, 4096
+    // own: 168, 156, 176).  They follow the lengths by powers of two: a recorded
+    // step is seldom recorded again.
+    const int live = (int)((total + longest - 1) / longest) * units;   // of as many windows as long as the longest
+    int fill = std::max(1, 256 / live), useful = 1;
+    for (int t = 2; t <= 4 && live > 256; ++t)
+      if (cdiv(live * t, 256) * fill < cdiv(live * fill, 256) * t) fill = t;
+    while (useful * 256 < longest) useful *= 2;
+    a.t_chunks = std::max(a.t_chunks, std::min({fill, useful, 1024 / (B * units)}));
+  }
+  a.t_chunks = std::min(a.t_chunks, cdiv(kv->max_len, 256));
   if (a.n_groups) {
     // a CU for each part of the prefix (31 instead of 32 chunks, to leave CUs
     // for those workgroups: 83 instead of 78 us at 32768 keys)
@@ -719,7 +753,8 @@ SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, 
 // one group, of two windows, makes the most chunks of a prefix.
 size_t share_parts(const dsi_model* m, const dsi_kv* kv, int B, int R) {
   const int queries = m->hq / m->hkv * R, tile = m->kvb ? 256 : 16;
-  const int own = std::max(1, 512 / (B * m->hkv * cdiv(queries, 16)));
+  const int units = m->hkv * cdiv(queries, 16);
+  const int own = std::max({1, 512 / (B * units), std::min(std::max(4, 256 / units), 1024 / (B * units))});
   const int prefix = B > 1 ? std::max(1, 256 / (m->hkv * cdiv(2 * queries, tile))) : 0;
   return (size_t)(std::min(prefix, cdiv(kv->max_len, 128)) + std::min(own, cdiv(kv->max_len, 256))) * B * R * m->hq;
 }
@@ -728,7 +763,7 @@ size_t share_parts(const dsi_model* m, const dsi_kv* kv, int B, int R) {
 // that is not possible (a captured call, no memory) the window kernels run, whose
 // buffers it has.
 bool share_forward(dsi_model* m, const SharePlan& p) {
-  if (!p.a.n_groups || m->share == 0 || (m->share < 0 && p.saved < kShareSaves)) return false;
+  if (!p.a.n_groups || m->share == 0 || (m->share < 0 && p.saved < kShareSaves + p.own / 4)) return false;
   return p.parts <= m->attn_parts || (!capturing(m) && ensure_attention(m, p.parts) == DSI_OK);
 }
 

@@ -10,7 +10,7 @@
 // The keys [0, s) are every row's, so the B R rows of a group are one product
 // without a mask, over one copy of the prefix; the rest is each window's own.
 // The first launch runs the prefix in chunks, and what a window has of its own
-// beyond its last kLast cached keys and the rows of the call (mostly nothing).
+// beyond its last kShareLast cached keys and the rows of the call (mostly nothing).
 // The second attends to those last keys and joins the parts: rows and masks are
 // its business alone, and no third launch reads what it computed.
 #include <limits.h>
@@ -24,7 +24,6 @@ namespace {
 
 constexpr int SW = 8;                  // waves per workgroup of the first launch
 constexpr int LW = 4;                  // and of the second
-constexpr int kLast = 256;             // cached keys that the second launch takes at most
 constexpr int kOwnChunk = SW * 32;     // keys of a window's own per workgroup of the first launch: a multiple of this
 
 __device__ __forceinline__ int wave_min(int v) {
@@ -64,7 +63,7 @@ __device__ __forceinline__ int own_chunk(int keys, int most) {
 }
 // keys [s, own_end) of a window of len cached positions are attended by the
 // first launch: whole blocks, all of them cached
-__device__ __forceinline__ int own_end(int s, int len) { return len - s <= kLast ? s : s + (len - s - 1) / kLast * kLast; }
+__device__ __forceinline__ int own_end(int s, int len) { return len - s <= kShareLast ? s : s + (len - s - 1) / kShareLast * kShareLast; }
 
 // Queries of one part: `rows` consecutive rows from row0 on, times the G query
 // heads of KV head kvh; query q is row q % rows of head q / rows.
@@ -662,9 +661,11 @@ __global__ __launch_bounds__(SW * 64) void k_share(ShareArgs a) {
   id -= n_prefix;
   const int kvh = id % a.n_kv;
   id /= a.n_kv;
-  const int win = id % a.B;
-  id /= a.B;
-  const int y = id % a.t_tiles, c = id / a.t_tiles;
+  // the windows of a row are turned by one each time: where B is a multiple of
+  // four, the few that have keys of their own would meet the same quarter of an
+  // XCD in every row (8 x 8 rows, two windows with 6000: 68 and 45 us)
+  const int row = id / a.B, win = (id + row) % a.B;
+  const int y = row % a.t_tiles, c = row / a.t_tiles;
   // no part of this launch reads the slots of the call's rows
   if (a.k_new && y == 0 && c == 0) append_rows<KVB, HD>(a, win, kvh);
   const int s = window_prefix(a, win);

@@ -164,6 +164,22 @@ def test_windows_of_their_own(dev):
         check(c, c.attend(0, 3, 4, q, k, v), 0, 4, lens, q, k, v)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,hd,windows,rows", [(8, 2, 64, 4, 3), (8, 8, 32, 8, 1), (16, 2, 128, 3, 5)])
+def test_long_continuations_and_a_window_beside_them(dev, kind, hq, hkv, hd, windows, rows):
+    """Keys of the windows' own in several chunks: some, all, and one window that shares nothing."""
+    prefix = 517
+    for tails, lone in (([0, 0, 2900, 0, 700], 0), ([257, 1025, 3001], 1800), ([3], 5000), ([300], 33)):
+        tails = [tails[i % len(tails)] for i in range(windows)]
+        n = max([prefix + t for t in tails] + [lone])
+        with Cache(hq, hkv, hd, kind, windows + 1, n + rows) as c:
+            lens = forked(c, 0, range(windows), prefix, tails) + [lone]
+            c.fill(windows, 0, lone)
+            dsi.dsi_kv_set_length(c.kv, windows, lone)
+            q, k, v = c.rows((windows + 1) * rows)
+            check(c, c.attend(0, windows + 1, rows, q, k, v), 0, rows, lens, q, k, v)
+
+
 def test_several_groups_and_a_root_outside_the_call(dev):
     with Cache(8, 2, 64, "bf16", 9, 1000) as c:
         lens = [0] * 9

@@ -264,6 +264,68 @@ def test_a_prefix_is_read_once_where_that_saves_enough(stub):
     ''')
 
 
+def test_keys_of_a_windows_own_are_cut_into_chunks(stub):
+    """One group in a call does not leave a long window, or a long continuation, to one workgroup a head."""
+    run(stub, '''
+    import os
+    os.environ["DSI_SHARE"] = "1"
+    def chunks(hq, hkv, rows, lens, shared, max_len=33000, grouped=True):
+        """workgroups per window, KV head and query tile in the first launch, besides the prefix's"""
+        m = dsi.dsi_model_create(dsi.make_config(1, 32, hq, hkv, 128, 32, 32, kvdtype=dsi.DSI_BF16), STREAM)
+        kv = dsi.dsi_kv_create(m, len(lens), max_len)
+        dsi.dsi_kv_set_length(kv, 0, max(shared))
+        for w in range(1, len(lens)):
+            if shared[w]:
+                dsi.dsi_kv_fork(kv, 0, w, 1, shared[w])
+        for w, n in enumerate(lens):
+            dsi.dsi_kv_set_length(kv, w, n)
+        hip.stub_clear()
+        dsi.dsi_attend(m, kv, 0, 0, len(lens), rows, P, P, P, P)
+        grid = [g[0] for k, _, g in launches() if k == "k_share"][0]
+        n = hq // hkv * rows * sum(s > 0 for s in shared)
+        tile = 256 if n > 128 else 128 if n > 64 else 64
+        prefix = hkv * -(-n // tile) * (256 // (hkv * -(-n // tile)))
+        t, rest = divmod(grid - prefix, len(lens) * hkv * -(-hq // hkv * rows // 16))
+        assert rest == 0
+        dsi.dsi_kv_destroy(kv)
+        dsi.dsi_model_destroy(m)
+        return t
+    # little of their own: few workgroups, most of which only cache rows
+    assert chunks(32, 8, 6, [8192] * 7, [8192] * 7) == 1
+    assert chunks(32, 8, 1, [8192] + [8400] * 3, [8192] * 4) == 4
+    # a window that shares nothing beside forked ones: 8 chunks and more of its 16384 keys
+    assert chunks(32, 8, 6, [8192] * 7 + [16384], [8192] * 7 + [0]) == 8
+    assert chunks(32, 8, 1, [8192] * 4 + [16384], [8192] * 4 + [0]) == 25
+    assert chunks(40, 40, 7, [2048] * 6 + [16384], [2048] * 6 + [0]) == 3
+    # continuations: one round of workgroups
+    assert chunks(32, 8, 6, [8192 + 4096] * 7, [8192] * 7) == 2
+    assert chunks(32, 8, 1, [8192 + 4096] * 8, [8192] * 8) == 4
+    assert chunks(32, 8, 6, [8192, 8192, 8192, 14000, 8192, 8192, 8192], [8192] * 7) == 9
+    assert chunks(40, 40, 1, [2048 + 4096] * 8, [2048] * 8) == 3          # 960 workgroups instead of 320, on 256 CUs
+    # no more than their keys fill
+    assert chunks(32, 8, 1, [8192 + 700] * 2, [8192] * 2) == 8 and chunks(32, 8, 6, [8192 + 700] * 2, [8192] * 2) == 4
+    ''')
+
+
+def test_windows_with_much_of_their_own_run_as_before(stub):
+    run(stub, '''
+    m = model(S.SHAPES["tiny"])
+    kv = dsi.dsi_kv_create(m, 6, 60000)
+    each = 2 * 4 * 32 * 4
+    dsi.dsi_profile_begin(m, dsi.DSI_K_ATTN)
+    for prefix in (14000, 20000):
+        spare = 5 * prefix - (64 << 20) // each            # positions
+        for own, want in ((0, True), (200, True), (4 * spare // 6 - 100, True), (4 * spare // 6 + 100, False), (30000, False)):
+            dsi.dsi_kv_set_length(kv, 0, prefix)
+            dsi.dsi_kv_fork(kv, 0, 1, 5)
+            for w in range(6):
+                dsi.dsi_kv_set_length(kv, w, prefix + own)
+            hip.stub_clear()
+            dsi.dsi_verify(m, kv, 0, 6, 1, P, P, P, P, P, commit=False)
+            assert ("k_share" in {k for k, _, _ in launches()}) == want, (prefix, own)
+    ''')
+
+
 def test_logprobs_refusals():
     lib = dsi.load()
     P = 4096
