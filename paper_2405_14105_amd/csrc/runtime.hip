@@ -667,6 +667,24 @@ void cut_shared(dsi_kv* kv, int window, long long len) {
     if (w == window || kv->root[w] == window) kv->shared[w] = std::min(kv->shared[w], len);
 }
 
+// How many readings of its prefix a group of n windows of R rows does without.
+// bf16: all but one.  fp32: a prefix is read once for 16 queries, one workgroup a
+// CU, so that what counts is the rounds of those.  In units of a window's reading
+// of its copy from memory (a 16-query tile of it from L2 costs 3/4), one such
+// reading of all CUs takes 2/3 (us a layer, by themselves and shared.  1B, 7 of 6:
+// 10922 positions, 105.7 and 102.0; 6 of 7: 13107, 100.3 and 119.2; 2 of 11: 32768,
+// 109.7 and 120.9; 8 of 8: 9362, 105.4 and 91.7; 8 of 1: 4681, 41.2 and 23.0.  8B, 16
+// of 4: 2184, 70.6 and 58.1; 4 of 8: 10922, 125.6 and 113.6; 3 of 4: 8192, 57.9 and
+// 50.9).  Below 512 positions the second launch costs more (13B, 6 of 7: 458
+// positions, 28.1 and 34.1, 655 37.9 and 37.5).
+double saved_copies(const dsi_model* m, int R, int n, long long common) {
+  if (m->kvb) return n - 1;
+  if (common < 512) return 0.0;
+  const int G = m->hq / m->hkv, wgs = m->hkv * cdiv(G * R * n, 16), chunks = std::max(1, 256 / wgs);
+  const double rounds = cdiv(wgs * chunks, 256) * 256.0 / (m->hkv * chunks);
+  return std::max(0.0, std::max((double)n, 0.75 * n * cdiv(G * R, 16)) - std::max(1.0, rounds * 2 / 3));
+}
+
 // The host knows which window each was forked from; how much of it is still
 // shared is known on the device when the attention runs, so the partition goes
 // by the cache's capacity.
@@ -696,7 +714,7 @@ SharePlan plan_shared(const dsi_model* m, const dsi_kv* kv, int window0, int B, 
       common = kv->max_len;
       for (int j = i; j < i + n; ++j)
         common = std::min(common, window0 + j == r ? kv->hi[r] : kv->shared[window0 + j]);
-      p.saved += (n - 1) * common * each;
+      p.saved += (size_t)(saved_copies(m, R, n, common) * common * each);
       common = common < kMinShared ? 0 : common / 32 * 32;
     }
     for (int j = i; j < i + n; ++j) {

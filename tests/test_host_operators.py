@@ -326,6 +326,38 @@ def test_windows_with_much_of_their_own_run_as_before(stub):
     ''')
 
 
+def test_an_fp32_prefix_is_shared_where_its_query_tiles_leave_something(stub):
+    """fp32 caches read a prefix once per 16 queries, one workgroup a CU: what is saved is counted from that."""
+    run(stub, '''
+    import dataclasses
+    def kernels(hq, hkv, hd, windows, rows, prefix, kind="f32"):
+        shape = dataclasses.replace(S.SHAPES["tiny"], n_layers=1, n_heads=hq, n_kv_heads=hkv, head_dim=hd, kvdtype=kind)
+        m = model(shape)
+        kv = dsi.dsi_kv_create(m, windows, prefix + 100)
+        dsi.dsi_kv_set_length(kv, 0, prefix)
+        dsi.dsi_kv_fork(kv, 0, 1, windows - 1)
+        dsi.dsi_profile_begin(m, dsi.DSI_K_ATTN)
+        hip.stub_clear()
+        dsi.dsi_verify(m, kv, 0, windows, rows - 1, P, P, P, P, P, commit=False)
+        k = {k for k, _, _ in launches()}
+        assert ("k_share" in k) != ("k_attn" in k)
+        dsi.dsi_kv_destroy(kv)
+        dsi.dsi_model_destroy(m)
+        return "k_share" in k
+    # 11 tiles of 16 queries make two rounds of the keys, as 16 would: nothing is gained
+    for prefix in (6553, 13107, 40000):
+        assert not kernels(32, 8, 64, 6, 7, prefix)
+        assert not kernels(32, 8, 128, 6, 7, prefix)
+        assert not kernels(32, 8, 64, 2, 11, prefix)
+        assert kernels(32, 8, 128, 6, 7, prefix, "bf16")
+    # one or two tiles for eight windows, and four rows each of sixteen
+    assert kernels(32, 8, 64, 8, 1, 4681) and kernels(32, 8, 128, 8, 1, 4681) and kernels(32, 8, 128, 16, 4, 2184)
+    assert kernels(32, 8, 128, 8, 8, 9362) and kernels(32, 8, 128, 3, 4, 16384)
+    # many KV heads: from 512 positions on
+    assert kernels(40, 40, 128, 6, 7, 655) and not kernels(40, 40, 128, 6, 7, 458) and not kernels(40, 40, 128, 16, 4, 218)
+    ''')
+
+
 def test_logprobs_refusals():
     lib = dsi.load()
     P = 4096
