@@ -9,6 +9,7 @@ import torch
 
 import dsi_synth as S
 from gpu_rig import Rig
+from share_cases import CASES
 from paper_2405_14105_amd import dsi
 
 pytestmark = pytest.mark.gpu
@@ -151,6 +152,24 @@ def test_row_counts(dev, windows, rows, hq, hkv, kind):
         lens = forked(c, 0, range(windows), 333, [(7 * b) % 29 for b in range(windows)])
         q, k, v = c.rows(windows * rows)
         check(c, c.attend(0, windows, rows, q, k, v), 0, rows, lens, q, k, v)
+
+
+@pytest.mark.parametrize("hq,hkv,hd,windows,rows,prefix,max_len,tiles,chunk", CASES)
+def test_variants_of_the_shared_prefix(dev, hq, hkv, hd, windows, rows, prefix, max_len, tiles, chunk):
+    with Cache(hq, hkv, hd, "bf16", windows, max_len) as c:
+        lens = forked(c, 0, range(windows), prefix, [(37 * b + 5) % 71 for b in range(windows)])
+        q, k, v = c.rows(windows * rows)
+        check(c, c.attend(0, windows, rows, q, k, v), 0, rows, lens, q, k, v)
+
+
+def test_three_groups_of_long_chunks(dev):
+    with Cache(32, 8, 128, "bf16", 8, 6200) as c:
+        lens = [0] * 8
+        for wins, n in (((0, 1, 2), 6001), ((3, 4), 3000), ((5, 6, 7), 4500)):
+            for w, x in zip(wins, forked(c, wins[0], wins, n, [11 * w % 37 for w in wins])):
+                lens[w] = x
+        q, k, v = c.rows(8 * 6)
+        check(c, c.attend(0, 8, 6, q, k, v), 0, 6, lens, q, k, v)
 
 
 def test_windows_of_their_own(dev):

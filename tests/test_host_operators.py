@@ -358,6 +358,37 @@ def test_an_fp32_prefix_is_shared_where_its_query_tiles_leave_something(stub):
     ''')
 
 
+def test_every_variant_of_the_shared_prefix_is_in_the_gpu_tests(stub):
+    """What the cases of share_cases.py launch, and that they leave out no variant that is built."""
+    run(stub, '''
+    sys.path.insert(0, "tests")
+    from share_cases import CASES
+    seen = set()
+    for hq, hkv, hd, windows, rows, prefix, max_len, tiles, chunk in CASES:
+        m = dsi.dsi_model_create(dsi.make_config(1, 32, hq, hkv, hd, 32, 32, kvdtype=dsi.DSI_BF16), STREAM)
+        kv = dsi.dsi_kv_create(m, windows, max_len)
+        dsi.dsi_kv_set_length(kv, 0, prefix)
+        dsi.dsi_kv_fork(kv, 0, 1, windows - 1)
+        hip.stub_clear()
+        dsi.dsi_attend(m, kv, 0, 0, windows, rows, P, P, P, P)
+        (name, args, grid), = [x for x in launches() if x[0] == "k_share"]
+        case = (hq, hkv, hd, windows, rows, prefix)
+        assert args == (1, hd, tiles), (case, args)
+        seen.add(args)
+        # the grid: chunks of the prefix as the kernel cuts them, and each window's first chunk
+        shared = prefix // 32 * 32
+        p_tiles = -(-hq // hkv * rows * windows // (32 * tiles))
+        p_chunks = min(256 // (hkv * p_tiles), -(-max_len // 128))
+        units = hkv * -(-hq // hkv * rows // 16)
+        assert grid[0] == hkv * p_tiles * p_chunks + windows * units * min(max(1, 128 // (windows * units)), -(-max_len // 256)), (case, grid)
+        least = 192 if tiles == 8 and shared > 2048 else 128
+        assert chunk == max(least, -(-(-(-shared // p_chunks)) // 64) * 64), case
+        dsi.dsi_kv_destroy(kv)
+        dsi.dsi_model_destroy(m)
+    assert seen == {a for k, a in built() if k == "k_share" and a[0] == 1}
+    ''')
+
+
 def test_logprobs_refusals():
     lib = dsi.load()
     P = 4096
