@@ -193,7 +193,7 @@ def score_continuations(target: int, kv: int, src: int, window0: int, w0: int, c
     # row i predicts token i of its continuation; -1: no token there
     targets = torch.tensor([[*c] + [-1] * (k + 1 - len(c)) for c in continuations], dtype=torch.int32, device=dev)
     rows = B * (k + 1)
-    n = torch.zeros((2, B), dtype=torch.int32, device=dev)
+    n = torch.empty((2, B), dtype=torch.int32, device=dev)   # not filled here: the model's stream writes it
     logits = torch.empty((rows, vocab), dtype=torch.float32, device=dev)
     lp, ent = (torch.empty((B, k + 1), dtype=torch.float32, device=dev) for _ in range(2))
     ids = torch.empty((B, k + 1, n_top), dtype=torch.int32, device=dev)
