@@ -109,7 +109,10 @@ enum {
  * bf16 layer and head weights are stored a second time in the order that
  * forwards of up to DSI_MAX_ROWS rows stream them, where the device has the
  * memory (about 16 GB at an 8B shape, 26 GB at 13B; d_model up to 5120).
- * DSI_RING=0, read here, does without. */
+ * DSI_RING=0, read here, does without.  DSI_SHARE, read here: 0 has dsi_verify
+ * and dsi_verify_tree read each window's own copy of a shared prefix
+ * (dsi_kv_fork), 1 the shared one from 128 positions on; by default they do
+ * where it saves enough. */
 dsi_status dsi_model_create(const dsi_config* cfg, void* stream, dsi_model** out);
 
 /* Upload one tensor (host memory if src_on_device == 0, else device memory).
@@ -302,10 +305,16 @@ dsi_status dsi_kv_wrap(dsi_model* m, int32_t n_windows, int32_t max_len, void* d
  * Stream-ordered; allocates nothing.
  * The library remembers which positions a window still has in common with the
  * window it was forked from: they end where either is rolled back, forked into
- * or imported to.  dsi_verify, dsi_verify_tree and dsi_attend read the
- * positions that consecutive windows of a call have in common with one
- * window (in the call or not) once for all of them, from 128 positions on.
- * Results then differ in rounding from those of a window by itself. */
+ * or imported to.  dsi_attend reads the positions that consecutive windows of a
+ * call have in common with the one window that they were forked from (in the
+ * call or not) once for all of them, from 128 positions on; fp32 caches once for
+ * every 16 query rows of a KV head.  Windows forked from different windows form
+ * different groups, whatever those have in common.  dsi_verify and
+ * dsi_verify_tree do so where it saves the reading of 64 MB of keys and values
+ * in a layer, and a quarter of what the windows have of their own; where a
+ * captured call or a shortage of memory leaves no room for it they run as for
+ * windows that were not forked.  Results then differ in rounding from those of
+ * a window by itself. */
 dsi_status dsi_kv_fork(dsi_kv* kv, int32_t src, int32_t window0, int32_t n_windows, int32_t len);
 
 /* Largest n_windows*rows of one dsi_attend. */
@@ -331,9 +340,13 @@ dsi_status dsi_kv_fork(dsi_kv* kv, int32_t src, int32_t window0, int32_t n_windo
  * DSI_ECAPACITY if a length + rows may exceed max_len.  A window whose rows no
  * longer fit when a captured call is replayed gets NaN, keeps its cache and
  * length, and is reported by the next synchronising call (DSI_EINVAL).
- * Numerics: fp32-accurate queries and probabilities against the cache's type,
- * fp32 sums.  A key or value of a row that is not finite reaches only the rows
- * that see it. */
+ * d_out overlaps none of the inputs.
+ * Numerics: fp32 scores, softmax statistics and sums.  With an fp32 cache
+ * everything is fp32.  With a bf16 cache each query and each probability enters
+ * its product as the sum of two bf16 numbers, which leaves 2^-18 of it: outputs
+ * are off by some 5e-6 of their size, where fp32 products leave 1e-6.
+ * A key or value that is not finite reaches only the rows that see it, and
+ * those are not finite where it has weight (an infinite value may become NaN). */
 typedef struct {
   int32_t layer, window0, n_windows, rows;
   const float* d_q;

@@ -433,7 +433,11 @@ hipError_t launch_fork_cut(const ForkState& f, int window, int new_len, hipStrea
 // share read once for all of them (share.hip).
 constexpr int kMaxForkGroups = kMaxRows / 2;
 constexpr int kMinShared = 128;   // a shorter shared prefix is read by each window
-constexpr int kShareLast = 256;   // cached keys of a window's own that the second launch takes at most
+// cached keys of a window's own that the second launch takes at most (a step, us,
+// with 128, 256 and 512: 13B, 6 x 7 rows, 180 keys of their own 35.6, 33.9, 33.8;
+// 400 40.1, 41.4, 38.6; windows that share nothing, 8B, 3 x 4 rows, 300 keys 16.6,
+// 16.7, 12.4, 1000 16.8, 17.6, 18.6, 4000 28.0, 29.2, 30.6)
+constexpr int kShareLast = 256;
 struct ShareGroup {
   int first, count;     // windows of the call
   int root;             // the window forked from

@@ -650,15 +650,17 @@ struct SharePlan {
 };
 
 // A forward reads a shared prefix once where that saves so much in a layer, and a
-// quarter of what its windows have of their own, which the window kernels read
-// faster (13B, 8 x 1 rows, 86 MB saved: with 671 MB of their own 128 us by themselves,
-// 147 shared, with 246 MB 77 and 74); below,
+// quarter of what its windows have of their own, which the window kernels mostly
+// read faster (us by themselves and shared.  13B, 8 x 1 rows, 147 MB saved, 1.3 GB of
+// their own: 250 and 282; 6 x 7, 70 MB and 503 MB: 103 and 114; 2 x 4, 70 and 61: 43
+// and 47; 8B, 4 x 4, 70 and 25: 38 and 46; but 7 x 6, 70 and 117: 71 and 59); below,
 // the window kernels are faster, whose workgroups are smaller and more (us a
-// layer, by themselves and shared.  8B, 7 windows of 6 rows: 2048 positions, 50
-// MB, 28.1 and 28.7; 4096 46.7 and 33.8; 32768 219 and 79; 2 of 11: 8192, 34 MB,
-// 32.5 and 35.5; 3 of 1: 4096, 34 MB, 21.5 and 25.2; 8192 36.8 and 27.7.  13B, 6 of
-// 7: 512, 52 MB, 17.6 and 23.3; 1024 27.4 and 26.5; 2048 61 and 30.  1B, 4 of 6:
-// 8192, 50 MB, 22.7 and 26.9; 32768 71 and 40)
+// layer of 16, by themselves and shared.  8B, 7 windows of 6 rows: 2048 positions,
+// 50 MB saved, 29.4 and 28.9; 4096 46.4 and 34.6; 32768 221 and 81; 2 of 11: 8192,
+// 34 MB, 34.5 and 36.1; 16384 50.8 and 42.8; 4 of 4: 6000, 74 MB, 32.3 and 36.0; 8192
+// 43.0 and 38.4; 3 of 1: 4096, 34 MB, 23.1 and 26.1; 8192 36.5 and 29.0.  13B, 6 of 7:
+// 668, 68 MB, 20.6 and 26.0; 1024 27.4 and 26.8; 2048 60.5 and 30.5; 8 of 1: 512, 73
+// MB, 25.5 and 25.7.  1B, 4 of 6: 8192, 50 MB, 24.6 and 27.6; 16384 40.0 and 32.0)
 constexpr size_t kShareSaves = (size_t)64 << 20;
 
 // a window's rows from len on may change from now on (fork_cut, on the device)

@@ -52,9 +52,10 @@ __device__ __forceinline__ int window_prefix(const ShareArgs& a, int win) {
 }
 // keys per chunk of a prefix: p_chunks chunks at most, of 128 keys at least, or
 // 192 where a part has up to 256 queries and the prefix over 2048 keys: a chunk
-// leaves HD * 4 bytes per query, which are read again (8B: 8 x 8 rows over 4096 keys
-// 40.6 us with 32 chunks of 128, 36.8 with 22 of 192; 7 x 6 over 2048 26.1 with 16
-// of 128, 28.2 with 11 of 192)
+// leaves HD * 4 bytes per query, which are read again, and up to 2048 keys there
+// are too few chunks for the CUs (a step, us, with 128 and 192: 8B, 8 x 8 rows over
+// 1024 keys 22.8 and 24.1, 2000 29.1 and 31.1, 2100 31.0 and 30.7, 3000 32.3 and
+// 31.8, 4096 38.6 and 35.0; 64 x 1 over 2048 37.2 and 38.7, 3500 48.6 and 44.4)
 __device__ __forceinline__ int prefix_chunk(const ShareArgs& a, int s) {
   return max(a.p_tile > 128 && s > 2048 ? 192 : 128, ((s + a.p_chunks - 1) / a.p_chunks + 63) & ~63);
 }
@@ -385,8 +386,8 @@ __device__ __forceinline__ f32x16 mfma32_bf16(const bf16x8& a, const bf16x8& b, 
 // wave, and KS = 8 / QT waves per tile that take the stage's 32-key blocks in
 // turn.  A stage's keys and values go through LDS once for all queries (two
 // stages, the next one's loads in flight in registers), so a CU takes in
-// HD * 128 bytes per 32 keys for 32 QT queries, and the matrix instructions
-// bound it from some 64 queries on.
+// HD * 128 bytes per 32 keys for 32 QT queries: from some 64 queries on computing
+// takes longer than that.
 // 32x32x16 MFMAs, S^T[key][query] = K Q^T and O^T[dim][query] += V^T P^T: lane l
 // holds query l % 32 in all of them.  Row rho of S^T stands for key
 // 16 (j >> 1) + 8 h + 4 (j & 1) + i of the block, rho = 8 j + 4 h + i, so that
@@ -401,11 +402,15 @@ __device__ __forceinline__ f32x16 mfma32_bf16(const bf16x8& a, const bf16x8& b, 
 // the window attention, which leaves 2^-18 of each: twice the products for an
 // error of 5e-6 of the output where fp32 sums leave 1e-6.  The running maximum
 // moves only when a score is 2^8 above it, so most blocks rescale nothing.
-// 256 queries over 32768 keys (8 KV heads of 128): 77 us, 0.9 PFLOP/s of these
-// products, where a library product of 8192^3 reaches 1.2 on the same card; 40 KV
-// heads with 42 queries over 8191 keys: 43 us, 5.5 TB/s once running, 16 us of it
-// launch, first loads, the waves' join and the partials' stores.  Four waves with
-// 64 queries each, a SIMD to themselves: 93 and 70 us.
+// 256 queries over 32768 keys (8 KV heads of 128): 79 us, 0.87 PFLOP/s of these
+// products, where a library product of 8192^3 reaches 1.2 on the same card.  The
+// matrix instructions are busy 38 % of that and the vector ones 31 %: the products
+// of the scores, the softmax and the products of the values of a block follow each
+// other, with two waves a SIMD to fill in.  40 KV heads with 42 queries over 8191
+// keys: 43 us, 5.5 TB/s once running, 16 us of it launch, first loads, the waves'
+// join and the partials' stores.  Four waves with 64 queries each, a SIMD to
+// themselves: 93 and 70 us.
+// An infinite value meets the zeros of low halves and gives NaN, whatever its weight.
 template <int HD, int QT>
 constexpr int tile_stage_blocks() { return SW / QT < 2 ? 2 : SW / QT; }
 template <int HD, int QT>
@@ -632,7 +637,8 @@ __device__ void append_rows(const ShareArgs& a, int win, int kvh) {
 }
 
 // First launch.  QT: query tiles of 32 per workgroup of the prefix's parts
-// (tile_part), or 0: 16 queries on the direct path (fp32 caches)
+// (tile_part), or 0: 16 queries on the direct path (fp32 caches, whose keys are
+// read again for every 16 queries)
 template <int KVB, int HD, int QT>
 __global__ __launch_bounds__(SW * 64) void k_share(ShareArgs a) {
   constexpr int kDirectLds = sizeof(WaveSums<SW, HD>);
@@ -676,8 +682,9 @@ __global__ __launch_bounds__(SW * 64) void k_share(ShareArgs a) {
 }
 
 // Bound by latency (launch, lengths, keys, partials: 6 us for 4 windows of one
-// row, 1B) or, where a group has many queries, by the partials: 256 queries and 32
-// chunks leave 33 MB, 17 us.
+// row, 1B) or, where a group has many queries, by the partials, eight of which are
+// loaded, waited for and joined at a time: 256 queries and 32 chunks leave 33 MB, 17
+// us, 2.3 TB/s.
 // Second launch: one workgroup per (window, KV head, 16 queries, VD dims) attends
 // to the window's last keys and the rows, and joins that with the partials of its
 // queries, in order.  Heads of more than 64 dims are halved: twice the workgroups
