@@ -29,9 +29,9 @@
  *  - Capacities (DSI_ECAPACITY) are checked against host bounds on the lengths,
  *    which are on the device.  A call that the caller captures into a graph of
  *    its own moves the bounds once, when it is captured, not when it is
- *    replayed.  After replays of calls that commit, append or fork,
- *    dsi_kv_length makes a window's bound its length; so does it before further
- *    calls on that window, and the caller replays only what fits.
+ *    replayed.  The caller replays only what fits, and after replays of calls
+ *    that commit, append or fork it calls dsi_kv_length, which makes a window's
+ *    bound its length, before other calls on that window.
  *  - A dsi_model's weights are immutable after they are set and the model
  *    may serve several dsi_kv; calls on one model (and its KV caches) must
  *    not overlap: the model's forward workspaces are shared by all of them.
@@ -345,8 +345,9 @@ dsi_status dsi_kv_fork(dsi_kv* kv, int32_t src, int32_t window0, int32_t n_windo
  * everything is fp32.  With a bf16 cache each query and each probability enters
  * its product as the sum of two bf16 numbers, which leaves 2^-18 of it: outputs
  * are off by some 5e-6 of their size, where fp32 products leave 1e-6.
- * A key or value that is not finite reaches only the rows that see it, and
- * those are not finite where it has weight (an infinite value may become NaN). */
+ * A key or value that is not finite reaches only the rows that see it; with a
+ * bf16 cache an infinite one may give NaN there where the formula gives a number
+ * or an infinity. */
 typedef struct {
   int32_t layer, window0, n_windows, rows;
   const float* d_q;
