@@ -244,6 +244,47 @@ def test_sharing_ends_with_rollback_import_and_fork(dev):
         again()
 
 
+@pytest.mark.parametrize("seed", range(4))
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_any_order_of_forks_and_cuts(dev, kind, seed):
+    """Random forks (of forks, over roots), rollbacks, imports and commits: every window's own cache is what it attends to."""
+    rng = np.random.default_rng(seed)
+    W, most, rows = 6, 1500, 2
+    with Cache(8, 2, 64, kind, W, most) as c:
+        lens = [0] * W
+        for step in range(40):
+            w = int(rng.integers(W))
+            op = rng.choice(["grow", "fork", "fork", "rollback", "import", "commit"])
+            if op == "grow":                     # positions behind the length are the window's alone
+                n = min(most - 64, lens[w] + int(rng.integers(1, 500)))
+                if n > lens[w]:
+                    c.fill(w, lens[w], n)
+                    dsi.dsi_kv_set_length(c.kv, w, n)
+                    lens[w] = n
+            elif op == "fork":
+                w0 = int(rng.integers(W))
+                n = int(rng.integers(1, W - w0 + 1))
+                if w < w0 or w >= w0 + n:
+                    length = int(rng.integers(0, lens[w] + 1)) if rng.random() < 0.5 else -1
+                    dsi.dsi_kv_fork(c.kv, w, w0, n, length)
+                    lens[w0:w0 + n] = [lens[w] if length < 0 else length] * n
+            elif op == "rollback":
+                lens[w] = int(rng.integers(0, lens[w] + 1))
+                dsi.dsi_kv_rollback(c.kv, w, lens[w])
+            elif op == "import" and lens[w]:
+                x = [c.rand(2, lens[w], 64).to(c.dt) for _ in range(2)]
+                dsi.dsi_kv_import(c.kv, w, 0, lens[w], *x)
+            w0 = int(rng.integers(W))
+            n = int(rng.integers(1, W - w0 + 1))
+            if max(lens[w0:w0 + n]) + rows > most:
+                continue
+            q, k, v = c.rows(n * rows)
+            check(c, c.attend(w0, n, rows, q, k, v, commit=op == "commit"), w0, rows, lens[w0:w0 + n], q, k, v)
+            if op == "commit":
+                lens[w0:w0 + n] = [x + rows for x in lens[w0:w0 + n]]
+        assert [dsi.dsi_kv_length(c.kv, w) for w in range(W)] == lens
+
+
 def test_rows_that_are_not_finite_reach_only_those_that_see_them(dev):
     for kind in ("bf16", "f32"):
         with Cache(8, 2, 64, kind, 2, 300) as c:
