@@ -400,6 +400,211 @@ typedef struct {
 dsi_status dsi_logprobs_workspace(int32_t rows, int32_t vocab, int32_t n_top, size_t* bytes);
 dsi_status dsi_logprobs(void* stream, const dsi_logprobs_args* args);
 
+/* ---- A server with projections of its own whose cache lies in pages --------
+ *
+ * The calls below take everything from the caller: no model, no handle.  They
+ * run on the stream given, allocate nothing, keep nothing past the call, may
+ * be captured into a graph, and may overlap where they share no output and no
+ * workspace.  The current device is the stream's.  Lengths, page tables and
+ * positions are read on the device when the work runs, so that a captured call
+ * may be replayed with others; whatever they hold, no memory outside the
+ * buffers that a call names is touched. */
+
+/* Which entries of a head a rotation turns together: HALF: j and j + dim/2;
+ * PAIRS: 2j and 2j + 1. */
+enum { DSI_ROPE_HALF = 0, DSI_ROPE_PAIRS = 1 };
+
+/* How the rotation's frequencies are stretched for contexts longer than a
+ * model was trained on (dsi_rope_table); f_j = base^(-2j / dim).
+ * PLAIN: f_j.  LINEAR: f_j / factor.  BASE: base' = base factor^(dim / (dim - 2)).
+ * BANDS: with c = context f_j / (2 pi) turns over the trained context, f_j from
+ *   `high` turns on, f_j / factor up to `low` turns, and between them
+ *   (1 - s) f_j / factor + s f_j, s = (c - low) / (high - low).
+ * RAMP (arXiv 2309.00071): the same mix by the pair's index, 1 - s rising from 0
+ *   to 1 between floor(j(high)) and ceil(j(low)), j(c) = dim ln(context / (2 pi c)) /
+ *   (2 ln base), these kept within [0, dim - 1]; rotated entries are multiplied
+ *   by 0.1 ln(factor) + 1. */
+enum { DSI_ROPE_PLAIN = 0, DSI_ROPE_LINEAR = 1, DSI_ROPE_BASE = 2, DSI_ROPE_BANDS = 3, DSI_ROPE_RAMP = 4 };
+typedef struct {
+  int32_t dim;          /* rotated entries of a head, even, 2..256 */
+  int32_t scaling;
+  double base;          /* > 1 */
+  double factor;        /* >= 1 (PLAIN: unused) */
+  double low, high;     /* BANDS, RAMP: 0 < low < high */
+  double context;       /* BANDS, RAMP: positions trained on, > 0 */
+} dsi_rope_spec;
+
+/* Host arithmetic only: freq [dim/2] (host memory) receives radians per
+ * position, *gain what rotated entries are multiplied by. */
+dsi_status dsi_rope_table(const dsi_rope_spec* spec, double* freq, float* gain);
+
+/* The rotation of position p: of each turned pair (a, b) and its frequency f,
+ * (a', b') = gain (a cos pf - b sin pf, b cos pf + a sin pf).  The first dim
+ * entries of each head are turned, the others kept.  Angles are formed in fp64. */
+typedef struct {
+  int32_t style;        /* DSI_ROPE_HALF or DSI_ROPE_PAIRS */
+  int32_t dim;          /* even, 0 (no rotation) .. head_dim */
+  const double* d_freq; /* [dim/2] device: radians per position */
+  float gain;           /* 1 without scaling */
+} dsi_rope;
+
+/* Norm and rotate the queries and keys of rows: what dsi_attend takes.
+ *   head_dim       a multiple of 32, at most 128
+ *   dtype          of d_q, d_k and the outputs (DSI_F32 or DSI_BF16); arithmetic
+ *                  in fp32, one rounding at the end
+ *   d_q, d_k       [rows][ld_q], [rows][ld_k]: a row's heads lie after each other,
+ *                  such as the parts of a fused projection's rows; each nullable
+ *                  with its output, n_heads or n_kv_heads then 0
+ *   d_pos          [rows] int32 (nullable with rope.dim = 0)
+ *   d_gain_q, _k   [head_dim] fp32, nullable: x is first divided by
+ *                  sqrt(mean(x^2) + eps) over its head and multiplied by the gain
+ *   d_q_out, d_k_out   [rows][ld_q_out], [rows][ld_k_out].  In place (the same
+ *                  pointer and stride) or apart from the input
+ * No alignment beyond the type's; 16-byte aligned pointers and strides, and a
+ * rope.dim that is a multiple of 16, are faster.  rows = 0 does nothing. */
+typedef struct {
+  int32_t rows, n_heads, n_kv_heads, head_dim, dtype;
+  int64_t ld_q, ld_k, ld_q_out, ld_k_out;
+  const void* d_q;
+  const void* d_k;
+  const int32_t* d_pos;
+  const float* d_gain_q;
+  const float* d_gain_k;
+  float eps;
+  dsi_rope rope;
+  void* d_q_out;
+  void* d_k_out;
+} dsi_rotate_args;
+
+dsi_status dsi_rotate(void* stream, const dsi_rotate_args* args);
+
+/* One layer of a cache in pages, and the rows of a step.
+ *   d_k, d_v       the pool of n_pages pages of page_size positions (a multiple
+ *                  of 32), 16-byte aligned, in kvdtype, in dsi_kv_wrap's blocks of
+ *                  32 positions: K [n_pages][n_kv_heads][page_size/32]
+ *                  [head_dim/32][32][32], the position before the dim, V
+ *                  [n_pages][n_kv_heads][page_size/32][head_dim][32]
+ *   d_table        [n_windows][max_pages] int32: the pages of a window, position
+ *                  p in entry p / page_size.  Windows may share pages that none of
+ *                  them appends to.  Entries that no row of a call needs may hold
+ *                  anything
+ *   d_len          [n_windows] int32: positions a window holds before the step
+ *   d_row0         [n_windows + 1] int32, ascending: rows d_row0[b] .. d_row0[b+1]-1
+ *                  of the step belong to window b, at positions d_len[b] ..; a
+ *                  window may have none.  Rows outside all of them are not
+ *                  touched, in any output
+ * The library changes neither lengths nor tables: the caller adds a step's rows
+ * to d_len after the step's last layer. */
+typedef struct {
+  int32_t n_kv_heads, head_dim, kvdtype, n_pages, page_size;
+  void* d_k;
+  void* d_v;
+  int32_t n_windows, max_pages;
+  const int32_t* d_table;
+  const int32_t* d_len;
+  const int32_t* d_row0;
+} dsi_pages;
+#define DSI_MAX_PAGE_WINDOWS 4096
+
+/* dsi_rotate of a step's rows, with the keys and the values rounded to kvdtype
+ * (nearest even) and put into the pages.  Rows beyond max_pages * page_size
+ * positions, or whose page is outside [0, n_pages), put nothing there.
+ *   d_q            nullable with d_q_out, n_heads then 0
+ *   d_v            [rows][ld_v], heads after each other
+ *   d_pos          [rows] int32, nullable: the positions rotated by, where they
+ *                  are not those of the cache (a token tree's depths) */
+typedef struct {
+  int32_t rows, n_heads, dtype;
+  int64_t ld_q, ld_k, ld_v, ld_q_out;
+  const void* d_q;
+  const void* d_k;
+  const void* d_v;
+  const int32_t* d_pos;
+  const float* d_gain_q;
+  const float* d_gain_k;
+  float eps;
+  dsi_rope rope;
+  void* d_q_out;
+} dsi_page_append_args;
+
+dsi_status dsi_page_append(void* stream, const dsi_pages* pages, const dsi_page_append_args* args);
+
+/* Attention of a step's rows over their windows' pages, the rows' own keys and
+ * values among them (dsi_page_append first): the row at position p of a window
+ * sees [max(0, p - reach + 1), p], or [0, p] with reach = 0, query head h reads KV
+ * head h / (n_heads / n_kv_heads), and out = softmax(scale q K^T) V.
+ *   dtype          of d_q and d_out (DSI_F32 or DSI_BF16)
+ *   d_q, d_out     [rows][ld_q], [rows][ld_out], heads after each other, 16-byte
+ *                  aligned rows; they do not overlap
+ *   scale          0: 1 / sqrt(head_dim)
+ *   d_ws           at least dsi_page_attend_workspace bytes, 16-byte aligned, for
+ *                  this call's work alone; what it holds does not matter
+ * A window with a negative length, with rows beyond max_pages * page_size
+ * positions, or with a page outside [0, n_pages) among those that a row sees: the
+ * row's outputs are NaN.  Positions that no row sees are never read into a result,
+ * whatever they hold, and pages that lie before every row's reach are not looked
+ * up.  Numerics: fp32 scores, softmax statistics and sums.  fp32 queries over a
+ * bf16 cache enter their products in three bf16 parts, probabilities too: fp32
+ * throughout.  bf16 queries: a probability is rounded to bf16 where a window has
+ * many rows, which doubles the output's own rounding error (2^-8 each), and to
+ * two bf16 parts where it has few.  A key or value that is not finite reaches only
+ * the rows that see it; an infinite one may give NaN there where the formula
+ * gives a number or an infinity. */
+typedef struct {
+  int32_t rows, n_heads, dtype, reach;
+  int64_t ld_q, ld_out;
+  const void* d_q;
+  float scale;
+  void* d_out;
+  void* d_ws;
+  size_t ws_bytes;
+} dsi_page_attend_args;
+
+dsi_status dsi_page_attend_workspace(const dsi_pages* pages, int32_t rows, int32_t n_heads, size_t* bytes);
+dsi_status dsi_page_attend(void* stream, const dsi_pages* pages, const dsi_page_attend_args* args);
+
+/* Penalties for tokens that were seen, biases, and a grammar's mask on rows of
+ * logits, before dsi_accept, dsi_logprobs or a sampler reads them.  For row i
+ * of window b, with c(v) the times that token v occurs among the window's
+ * n_seen tokens and the first i + 1 of its row tokens, and in this order:
+ *   c > 0: z = z > 0 ? z / repetition : z * repetition
+ *   z = z - frequency c - (c > 0 ? presence : 0)
+ *   z = z + bias(v);  z = -inf where v is not allowed
+ * so that every row of a verified window is judged by the text it continues.
+ *   d_logits       [n_windows*rows][ld], d_out [n_windows*rows][ld_out], entries
+ *                  of type dtype; in place (the same pointer and stride; only
+ *                  what changes, and its neighbours within 16 bytes, is then
+ *                  written) or apart
+ *   d_seen         [n_windows][ld_seen] int32, ld_seen + rows < 2^21, and d_n_seen
+ *                  [n_windows] int32, kept within [0, ld_seen]; nullable together
+ *   d_tokens       [n_windows][rows] int32, nullable: the row tokens (w0, d_1 ..
+ *                  d_k of dsi_verify)
+ *   d_repetition, d_frequency, d_presence   [n_windows] fp32, each nullable (1, 0, 0)
+ *   d_bias_ids, d_bias   [n_windows][n_bias], n_bias <= 1024; the last entry of
+ *                  an id counts
+ *   d_allowed      [n_windows*rows][ld_allowed] words, nullable: token v is
+ *                  allowed if bit v % 32 of word v / 32 is set
+ * Ids outside [0, vocab) (such as -1 for padding) are passed over.  Arithmetic
+ * in fp32, one rounding to dtype at the end.  rows *
+ * n_windows = 0 does nothing. */
+typedef struct {
+  int32_t n_windows, rows, vocab, dtype, n_bias;
+  int64_t ld, ld_out, ld_seen, ld_allowed;
+  const void* d_logits;
+  const int32_t* d_seen;
+  const int32_t* d_n_seen;
+  const int32_t* d_tokens;
+  const float* d_repetition;
+  const float* d_frequency;
+  const float* d_presence;
+  const int32_t* d_bias_ids;
+  const float* d_bias;
+  const uint32_t* d_allowed;
+  void* d_out;
+} dsi_adjust_args;
+
+dsi_status dsi_adjust(void* stream, const dsi_adjust_args* args);
+
 /* Roll a window back to new_len (DSI terminates the threads that built on a
  * rejected token, Algorithm 1; their cache rows become dead).  Stream-ordered;
  * new_len must be >= 0 and not above the window's current length (checked on

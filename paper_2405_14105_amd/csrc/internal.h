@@ -472,6 +472,88 @@ int share_tile(int kv_bf16, int queries);
 hipError_t launch_attention_shared(int kv_bf16, int hd, const ShareArgs& a, hipStream_t s);
 hipError_t launch_kv_advance(int* lens, int window0, int B, int rows, int max_len, hipStream_t s);
 
+// limits of the calls on pages (dsi_rotate and on): positions and entries of a
+// step stay far from 32 bits, offsets into tensors are 64-bit
+constexpr int kMaxStepRows = 1 << 22;
+constexpr int kMaxStepHeads = 1024;
+constexpr int kMaxStepPositions = 1 << 30;
+constexpr int kMaxStepQueries = 1 << 28;   // of a KV head
+constexpr long long kMaxStepLd = 1ll << 40;
+constexpr int kMaxBias = 1024;          // dsi_adjust: entries of a window's biases,
+constexpr int kMaxCount = 1 << 21;      // and tokens that a row has seen
+// A layer of a cache in pages and the rows of a step (rotate.hip, pages.hip):
+// everything on the device is the caller's and checked where it is used.
+struct PageArgs {
+  int nkv, hd, kvb;     // kvb: bf16 (otherwise fp32)
+  int n_pages, bpp;     // blocks of 32 positions in a page
+  int n_windows;        // 0: no pages (dsi_rotate)
+  int max_pages;
+  void* k;
+  void* v;
+  const int* table;
+  const int* len;
+  const int* row0;
+};
+// Rotation of queries and keys, and their way into the pages (rotate.hip)
+struct RotateArgs {
+  int rows, nq, nk, nv, hd, bf16;
+  size_t ldq, ldk, ldv, ldqo, ldko;   // entries
+  const void* q;
+  const void* k;
+  const void* v;
+  const int* pos;       // nullable with pages, and with dim = 0
+  const float* gq;
+  const float* gk;
+  float eps;
+  int style, dim;       // style 1: pairs
+  const double* freq;
+  float gain;
+  void* qo;
+  void* ko;             // unused with pages
+  PageArgs pg;
+  int passes, ppw, wpr; // head groups of a row, a wave's, and waves per row
+  int row_blocks;       // workgroups of queries and keys; the others take values
+};
+hipError_t launch_rotate(RotateArgs a, bool wide, hipStream_t s);
+
+// Attention of a step's rows over pages (pages.hip)
+struct PageAttnArgs {
+  PageArgs pg;
+  int rows, nq, bf16, reach;   // bf16: queries and outputs
+  size_t ldq, ldo;
+  const void* q;
+  void* out;
+  float scale2;         // scale * log2 e
+  // one class of windows: those with qlo..qhi queries of a KV head
+  int qlo, qhi;
+  int tile;             // queries per tile
+  int target;           // items (of all KV heads) a launch is cut into where its windows are long
+  int least;            // units of keys an item has at least
+  float* part;          // [slots][head_dim][tile]
+  float2* ml;           // [slots][tile]: maximum (base 2) and sum
+};
+size_t page_attend_workspace_bytes(const PageArgs& pg, int rows, int nq);
+hipError_t launch_page_attend(PageAttnArgs a, void* ws, hipStream_t s);
+
+// Penalties, biases and masks on rows of logits (adjust.hip)
+struct AdjustArgs {
+  int B, R, V, bf16, n_bias;
+  size_t ld, ldo, ldseen, lda;
+  const void* z;
+  void* out;            // = z: in place
+  const int* seen;
+  const int* n_seen;
+  const int* tokens;
+  const float* repetition;
+  const float* frequency;
+  const float* presence;
+  const int* bias_ids;
+  const float* bias;
+  const uint32_t* allowed;
+  int chunks, groups, rpg;   // of a window: vocabulary chunks, groups of rpg rows
+};
+hipError_t launch_adjust(AdjustArgs a, hipStream_t s);
+
 // KV and misc (elementwise.hip)
 hipError_t launch_kv_rollback(const ForkState& f, int window, int new_len, int* err, hipStream_t s);
 hipError_t launch_kv_set(const ForkState& f, int window, int new_len, hipStream_t s);

@@ -2130,6 +2130,295 @@ dsi_status dsi_logprobs(void* stream, const dsi_logprobs_args* a) {
   return DSI_OK;
 }
 
+dsi_status dsi_rope_table(const dsi_rope_spec* s, double* freq, float* gain) {
+  if (!s || !freq || !gain) return fail(DSI_EINVAL, "null argument");
+  if (s->dim < 2 || s->dim > 256 || s->dim % 2) return fail(DSI_EINVAL, "dim must be even, in [2, 256]");
+  if (s->scaling < DSI_ROPE_PLAIN || s->scaling > DSI_ROPE_RAMP) return fail(DSI_EINVAL, "bad scaling %d", s->scaling);
+  if (!(s->base > 1.0) || !std::isfinite(s->base)) return fail(DSI_EINVAL, "base must be above 1");
+  const bool scaled = s->scaling != DSI_ROPE_PLAIN, mixed = s->scaling == DSI_ROPE_BANDS || s->scaling == DSI_ROPE_RAMP;
+  if (scaled && (!(s->factor >= 1.0) || !std::isfinite(s->factor))) return fail(DSI_EINVAL, "factor must be >= 1");
+  if (s->scaling == DSI_ROPE_BASE && s->dim < 4) return fail(DSI_EINVAL, "a scaled base needs dim >= 4");
+  if (mixed && (!(s->low > 0.0) || !(s->high > s->low) || !std::isfinite(s->high)))
+    return fail(DSI_EINVAL, "low and high must satisfy 0 < low < high");
+  if (mixed && (!(s->context > 0.0) || !std::isfinite(s->context))) return fail(DSI_EINVAL, "context must be positive");
+  const double two_pi = 6.283185307179586477;
+  const int dim = s->dim;
+  double base = s->base, lo = 0.0, hi = 0.0;
+  if (s->scaling == DSI_ROPE_BASE) base *= std::pow(s->factor, dim / (dim - 2.0));
+  if (s->scaling == DSI_ROPE_RAMP) {
+    auto index = [&](double turns) { return dim * std::log(s->context / (two_pi * turns)) / (2.0 * std::log(base)); };
+    lo = std::min(std::max(std::floor(index(s->high)), 0.0), dim - 1.0);
+    hi = std::min(std::max(std::ceil(index(s->low)), 0.0), dim - 1.0);
+  }
+  for (int j = 0; j < dim / 2; ++j) {
+    double f = std::pow(base, -2.0 * j / dim);
+    double slow = 0.0;   // share of the stretched frequency
+    if (s->scaling == DSI_ROPE_LINEAR) slow = 1.0;
+    if (s->scaling == DSI_ROPE_BANDS)
+      slow = 1.0 - std::min(std::max((s->context * f / two_pi - s->low) / (s->high - s->low), 0.0), 1.0);
+    if (s->scaling == DSI_ROPE_RAMP) slow = std::min(std::max((j - lo) / std::max(hi - lo, 0.001), 0.0), 1.0);
+    if (slow > 0.0) f = slow * f / s->factor + (1.0 - slow) * f;
+    freq[j] = f;
+  }
+  *gain = s->scaling == DSI_ROPE_RAMP ? (float)(0.1 * std::log(s->factor) + 1.0) : 1.f;
+  return DSI_OK;
+}
+
+static bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
+// rows of `heads` heads, ld entries apart
+static dsi_status rows_ok(const char* what, const void* p, int64_t ld, long long entries, size_t esz) {
+  if (!p) return fail(DSI_EINVAL, "null %s", what);
+  if (!aligned(p, esz)) return fail(DSI_EINVAL, "misaligned %s", what);
+  if (ld < entries || ld > kMaxStepLd)
+    return fail(DSI_EINVAL, "%s: rows of %lld entries lie %lld apart", what, entries, (long long)ld);
+  return DSI_OK;
+}
+// in place, or apart
+static dsi_status apart_ok(const char* what, const void* in, int64_t ld_in, const void* out, int64_t ld_out, int rows,
+                           long long entries, size_t esz) {
+  if (in == out && ld_in == ld_out) return DSI_OK;
+  const uintptr_t i0 = (uintptr_t)in, o0 = (uintptr_t)out;
+  const uintptr_t i1 = i0 + ((size_t)(rows - 1) * ld_in + entries) * esz, o1 = o0 + ((size_t)(rows - 1) * ld_out + entries) * esz;
+  if (i0 < o1 && o0 < i1) return fail(DSI_EINVAL, "%s overlaps its output without being in place", what);
+  return DSI_OK;
+}
+
+static dsi_status rope_ok(const dsi_rope& r, int hd) {
+  if (r.dim < 0 || r.dim > hd || r.dim % 2) return fail(DSI_EINVAL, "rope.dim must be even, in [0, %d]", hd);
+  if (!r.dim) return DSI_OK;
+  if (r.style != DSI_ROPE_HALF && r.style != DSI_ROPE_PAIRS) return fail(DSI_EINVAL, "bad rope.style %d", r.style);
+  if (!r.d_freq || !aligned(r.d_freq, 8)) return fail(DSI_EINVAL, "null or misaligned frequencies");
+  if (!std::isfinite(r.gain)) return fail(DSI_EINVAL, "rope.gain must be finite");
+  return DSI_OK;
+}
+
+// what dsi_rotate and dsi_page_append share; q, k and their outputs are checked
+static dsi_status rotate_args(RotateArgs& r, int rows, int nq, int nk, int hd, int dtype, const void* d_pos, const void* gq,
+                              const void* gk, float eps, const dsi_rope& rope) {
+  if (rows < 0 || rows > kMaxStepRows) return fail(DSI_EINVAL, "rows must be in [0, %d]", kMaxStepRows);
+  if (nq < 0 || nk < 0 || nq > kMaxStepHeads || nk > kMaxStepHeads) return fail(DSI_EINVAL, "heads must be in [0, %d]", kMaxStepHeads);
+  if (hd < 32 || hd > 128 || hd % 32) return fail(DSI_EINVAL, "head_dim must be a multiple of 32, at most 128");
+  if (dtype != DSI_F32 && dtype != DSI_BF16) return fail(DSI_EINVAL, "bad dtype %d", dtype);
+  DSI_TRY(rope_ok(rope, hd));
+  if ((gq || gk) && (!(eps >= 0.f) || !std::isfinite(eps))) return fail(DSI_EINVAL, "eps must be >= 0");
+  if (!aligned(gq, 4) || !aligned(gk, 4) || !aligned(d_pos, 4)) return fail(DSI_EINVAL, "misaligned gains or positions");
+  r.rows = rows;
+  r.nq = nq;
+  r.nk = nk;
+  r.hd = hd;
+  r.bf16 = dtype == DSI_BF16;
+  r.pos = (const int*)d_pos;
+  r.gq = (const float*)gq;
+  r.gk = (const float*)gk;
+  r.eps = eps;
+  r.style = rope.style == DSI_ROPE_PAIRS && rope.dim;
+  r.dim = rope.dim;
+  r.freq = rope.d_freq;
+  r.gain = rope.gain;
+  return DSI_OK;
+}
+// whether 16-byte pieces fit the rows at p, ld entries apart
+static bool wide_rows(const void* p, size_t ld, size_t esz) { return aligned(p, 16) && ld * esz % 16 == 0; }
+
+dsi_status dsi_rotate(void* stream, const dsi_rotate_args* a) {
+  if (!a) return fail(DSI_EINVAL, "null argument");
+  RotateArgs r{};
+  DSI_TRY(rotate_args(r, a->rows, a->n_heads, a->n_kv_heads, a->head_dim, a->dtype, a->d_pos, a->d_gain_q, a->d_gain_k, a->eps,
+                      a->rope));
+  if (!a->rows || a->n_heads + a->n_kv_heads == 0) return DSI_OK;
+  if (a->rope.dim && !a->d_pos) return fail(DSI_EINVAL, "null positions");
+  const size_t esz = r.bf16 ? 2 : 4;
+  bool wide = r.style || r.dim % (32 / (int)esz) == 0;
+  auto part = [&](const char* what, int heads, const void* in, int64_t ld, void* out, int64_t ld_out) -> dsi_status {
+    if (!heads) return DSI_OK;
+    const long long n = (long long)heads * a->head_dim;
+    DSI_TRY(rows_ok(what, in, ld, n, esz));
+    DSI_TRY(rows_ok(what, out, ld_out, n, esz));
+    DSI_TRY(apart_ok(what, in, ld, out, ld_out, a->rows, n, esz));
+    wide = wide && wide_rows(in, ld, esz) && wide_rows(out, ld_out, esz);
+    return DSI_OK;
+  };
+  DSI_TRY(part("queries", a->n_heads, a->d_q, a->ld_q, a->d_q_out, a->ld_q_out));
+  DSI_TRY(part("keys", a->n_kv_heads, a->d_k, a->ld_k, a->d_k_out, a->ld_k_out));
+  r.q = a->d_q;
+  r.k = a->d_k;
+  r.qo = a->d_q_out;
+  r.ko = a->d_k_out;
+  r.ldq = (size_t)a->ld_q;
+  r.ldk = (size_t)a->ld_k;
+  r.ldqo = (size_t)a->ld_q_out;
+  r.ldko = (size_t)a->ld_k_out;
+  HIP_TRY(launch_rotate(r, wide, (hipStream_t)stream));
+  return DSI_OK;
+}
+
+static dsi_status pages_ok(const dsi_pages* p, PageArgs& o) {
+  if (!p) return fail(DSI_EINVAL, "null pages");
+  if (p->n_kv_heads < 1 || p->n_kv_heads > kMaxStepHeads) return fail(DSI_EINVAL, "n_kv_heads must be in [1, %d]", kMaxStepHeads);
+  if (p->head_dim < 32 || p->head_dim > 128 || p->head_dim % 32) return fail(DSI_EINVAL, "head_dim must be a multiple of 32, at most 128");
+  if (p->kvdtype != DSI_F32 && p->kvdtype != DSI_BF16) return fail(DSI_EINVAL, "bad kvdtype %d", p->kvdtype);
+  if (p->n_pages < 1) return fail(DSI_EINVAL, "n_pages must be >= 1");
+  if (p->page_size < 32 || p->page_size % 32) return fail(DSI_EINVAL, "page_size must be a positive multiple of 32");
+  if (p->max_pages < 1 || (long long)p->max_pages * p->page_size > kMaxStepPositions)
+    return fail(DSI_EINVAL, "max_pages * page_size must be in [1, %d]", kMaxStepPositions);
+  if (p->n_windows < 1 || p->n_windows > DSI_MAX_PAGE_WINDOWS)
+    return fail(DSI_EINVAL, "n_windows must be in [1, %d]", DSI_MAX_PAGE_WINDOWS);
+  if ((long long)p->n_pages * p->n_kv_heads * (p->page_size / 32) > INT_MAX)
+    return fail(DSI_EINVAL, "n_pages * n_kv_heads * page_size / 32 exceeds %d", INT_MAX);
+  o.nkv = p->n_kv_heads;
+  o.hd = p->head_dim;
+  o.kvb = p->kvdtype == DSI_BF16;
+  o.n_pages = p->n_pages;
+  o.bpp = p->page_size / 32;
+  o.n_windows = p->n_windows;
+  o.max_pages = p->max_pages;
+  o.k = p->d_k;
+  o.v = p->d_v;
+  o.table = p->d_table;
+  o.len = p->d_len;
+  o.row0 = p->d_row0;
+  return DSI_OK;
+}
+static dsi_status page_pointers_ok(const dsi_pages* p) {
+  if (!p->d_k || !p->d_v || !aligned(p->d_k, 16) || !aligned(p->d_v, 16)) return fail(DSI_EINVAL, "null or misaligned pages");
+  if (!p->d_table || !p->d_len || !p->d_row0 || !aligned(p->d_table, 4) || !aligned(p->d_len, 4) || !aligned(p->d_row0, 4))
+    return fail(DSI_EINVAL, "null or misaligned table, lengths or rows of the windows");
+  return DSI_OK;
+}
+
+dsi_status dsi_page_append(void* stream, const dsi_pages* pages, const dsi_page_append_args* a) {
+  if (!a) return fail(DSI_EINVAL, "null argument");
+  RotateArgs r{};
+  DSI_TRY(pages_ok(pages, r.pg));
+  DSI_TRY(rotate_args(r, a->rows, a->n_heads, pages->n_kv_heads, pages->head_dim, a->dtype, a->d_pos, a->d_gain_q, a->d_gain_k,
+                      a->eps, a->rope));
+  if (!a->rows) return DSI_OK;
+  DSI_TRY(page_pointers_ok(pages));
+  const size_t esz = r.bf16 ? 2 : 4;
+  const long long nq = (long long)a->n_heads * r.hd, nk = (long long)r.nk * r.hd;
+  bool wide = r.style || r.dim % (32 / (int)esz) == 0;
+  if (a->n_heads) {
+    DSI_TRY(rows_ok("queries", a->d_q, a->ld_q, nq, esz));
+    DSI_TRY(rows_ok("output", a->d_q_out, a->ld_q_out, nq, esz));
+    DSI_TRY(apart_ok("queries", a->d_q, a->ld_q, a->d_q_out, a->ld_q_out, a->rows, nq, esz));
+    wide = wide && wide_rows(a->d_q, a->ld_q, esz) && wide_rows(a->d_q_out, a->ld_q_out, esz);
+  }
+  DSI_TRY(rows_ok("keys", a->d_k, a->ld_k, nk, esz));
+  DSI_TRY(rows_ok("values", a->d_v, a->ld_v, nk, esz));
+  wide = wide && wide_rows(a->d_k, a->ld_k, esz) && wide_rows(a->d_v, a->ld_v, esz);
+  r.nv = r.nk;
+  r.q = a->d_q;
+  r.k = a->d_k;
+  r.v = a->d_v;
+  r.qo = a->d_q_out;
+  r.ldq = (size_t)a->ld_q;
+  r.ldk = (size_t)a->ld_k;
+  r.ldv = (size_t)a->ld_v;
+  r.ldqo = (size_t)a->ld_q_out;
+  HIP_TRY(launch_rotate(r, wide, (hipStream_t)stream));
+  return DSI_OK;
+}
+
+static dsi_status page_attend_sizes_ok(const dsi_pages* pages, int32_t rows, int32_t n_heads, PageArgs& p) {
+  DSI_TRY(pages_ok(pages, p));
+  if (rows < 0 || rows > kMaxStepRows) return fail(DSI_EINVAL, "rows must be in [0, %d]", kMaxStepRows);
+  if (n_heads < 1 || n_heads > kMaxStepHeads || n_heads % p.nkv)
+    return fail(DSI_EINVAL, "n_heads must be a multiple of n_kv_heads, at most %d", kMaxStepHeads);
+  if ((long long)rows * (n_heads / p.nkv) > kMaxStepQueries)
+    return fail(DSI_EINVAL, "rows * n_heads / n_kv_heads exceeds %d", kMaxStepQueries);
+  return DSI_OK;
+}
+
+dsi_status dsi_page_attend_workspace(const dsi_pages* pages, int32_t rows, int32_t n_heads, size_t* bytes) {
+  if (!bytes) return fail(DSI_EINVAL, "null argument");
+  PageArgs p{};
+  DSI_TRY(page_attend_sizes_ok(pages, rows, n_heads, p));
+  *bytes = rows ? page_attend_workspace_bytes(p, rows, n_heads) : 0;
+  return DSI_OK;
+}
+
+dsi_status dsi_page_attend(void* stream, const dsi_pages* pages, const dsi_page_attend_args* a) {
+  if (!a) return fail(DSI_EINVAL, "null argument");
+  PageAttnArgs d{};
+  DSI_TRY(page_attend_sizes_ok(pages, a->rows, a->n_heads, d.pg));
+  if (a->dtype != DSI_F32 && a->dtype != DSI_BF16) return fail(DSI_EINVAL, "bad dtype %d", a->dtype);
+  if (a->reach < 0) return fail(DSI_EINVAL, "reach must be >= 0");
+  if (!(a->scale >= 0.f) || !std::isfinite(a->scale)) return fail(DSI_EINVAL, "scale must be >= 0");
+  if (!a->rows) return DSI_OK;
+  DSI_TRY(page_pointers_ok(pages));
+  const size_t esz = a->dtype == DSI_BF16 ? 2 : 4;
+  const long long n = (long long)a->n_heads * pages->head_dim;
+  DSI_TRY(rows_ok("queries", a->d_q, a->ld_q, n, esz));
+  DSI_TRY(rows_ok("output", a->d_out, a->ld_out, n, esz));
+  if (!wide_rows(a->d_q, (size_t)a->ld_q, esz) || !wide_rows(a->d_out, (size_t)a->ld_out, esz))
+    return fail(DSI_EINVAL, "rows of queries and output must be 16-byte aligned");
+  if (a->d_q == a->d_out) return fail(DSI_EINVAL, "d_out overlaps d_q");
+  DSI_TRY(apart_ok("queries", a->d_q, a->ld_q, a->d_out, a->ld_out, a->rows, n, esz));
+  const size_t need = page_attend_workspace_bytes(d.pg, a->rows, a->n_heads);
+  if (!a->d_ws || !aligned(a->d_ws, 16) || a->ws_bytes < need)
+    return fail(DSI_EINVAL, "the workspace must hold %zu bytes, 16-byte aligned (got %zu)", need, a->ws_bytes);
+  d.rows = a->rows;
+  d.nq = a->n_heads;
+  d.bf16 = a->dtype == DSI_BF16;
+  d.reach = a->reach;
+  d.ldq = (size_t)a->ld_q;
+  d.ldo = (size_t)a->ld_out;
+  d.q = a->d_q;
+  d.out = a->d_out;
+  d.scale2 = (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)pages->head_dim)) * 1.44269504088896340736f;
+  HIP_TRY(launch_page_attend(d, a->d_ws, (hipStream_t)stream));
+  return DSI_OK;
+}
+
+dsi_status dsi_adjust(void* stream, const dsi_adjust_args* a) {
+  if (!a) return fail(DSI_EINVAL, "null argument");
+  if (a->n_windows < 0 || a->rows < 0 || (long long)a->n_windows * a->rows > kMaxStepRows)
+    return fail(DSI_EINVAL, "n_windows*rows must be in [0, %d]", kMaxStepRows);
+  if (a->vocab < 1 || a->vocab > kMaxLogprobVocab) return fail(DSI_EINVAL, "vocab must be in [1, %d]", kMaxLogprobVocab);
+  if (a->dtype != DSI_F32 && a->dtype != DSI_BF16) return fail(DSI_EINVAL, "bad dtype %d", a->dtype);
+  if (a->n_bias < 0 || a->n_bias > kMaxBias) return fail(DSI_EINVAL, "n_bias must be in [0, %d]", kMaxBias);
+  if (!a->d_seen != !a->d_n_seen) return fail(DSI_EINVAL, "d_seen and d_n_seen come together");
+  if (a->d_seen && (a->ld_seen < 1 || a->ld_seen + a->rows >= kMaxCount))
+    return fail(DSI_EINVAL, "ld_seen must be positive, ld_seen + rows below %d", kMaxCount);
+  if (a->rows >= kMaxCount) return fail(DSI_EINVAL, "rows must be below %d", kMaxCount);
+  if (!a->n_windows || !a->rows) return DSI_OK;
+  if ((long long)a->n_windows * a->rows * a->vocab > kMaxStepLd) return fail(DSI_EINVAL, "n_windows*rows*vocab exceeds %lld", kMaxStepLd);
+  const size_t esz = a->dtype == DSI_BF16 ? 2 : 4;
+  DSI_TRY(rows_ok("logits", a->d_logits, a->ld, a->vocab, esz));
+  DSI_TRY(rows_ok("output", a->d_out, a->ld_out, a->vocab, esz));
+  DSI_TRY(apart_ok("logits", a->d_logits, a->ld, a->d_out, a->ld_out, a->n_windows * a->rows, a->vocab, esz));
+  if (a->n_bias && (!a->d_bias_ids || !a->d_bias)) return fail(DSI_EINVAL, "null biases");
+  if (a->d_allowed && (a->ld_allowed < ((int64_t)a->vocab + 31) / 32 || a->ld_allowed > kMaxStepLd))
+    return fail(DSI_EINVAL, "ld_allowed %lld below the vocabulary's words", (long long)a->ld_allowed);
+  for (const void* p : {(const void*)a->d_seen, (const void*)a->d_n_seen, (const void*)a->d_tokens, (const void*)a->d_repetition,
+                        (const void*)a->d_frequency, (const void*)a->d_presence, (const void*)a->d_bias_ids,
+                        (const void*)a->d_bias, (const void*)a->d_allowed})
+    if (!aligned(p, 4)) return fail(DSI_EINVAL, "misaligned argument");
+  AdjustArgs d{};
+  d.B = a->n_windows;
+  d.R = a->rows;
+  d.V = a->vocab;
+  d.bf16 = a->dtype == DSI_BF16;
+  d.n_bias = a->n_bias;
+  d.ld = (size_t)a->ld;
+  d.ldo = (size_t)a->ld_out;
+  d.ldseen = (size_t)a->ld_seen;
+  d.lda = (size_t)a->ld_allowed;
+  d.z = a->d_logits;
+  d.out = a->d_out;
+  d.seen = a->d_seen;
+  d.n_seen = a->d_n_seen;
+  d.tokens = a->d_tokens;
+  d.repetition = a->d_repetition;
+  d.frequency = a->d_frequency;
+  d.presence = a->d_presence;
+  d.bias_ids = a->d_bias_ids;
+  d.bias = a->d_bias;
+  d.allowed = a->d_allowed;
+  HIP_TRY(launch_adjust(d, (hipStream_t)stream));
+  return DSI_OK;
+}
+
 dsi_status dsi_kv_rollback(dsi_kv* kv, int32_t window, int32_t new_len) {
   if (!kv) return fail(DSI_EINVAL, "null kv");
   if (window < 0 || window >= kv->n_windows) return fail(DSI_EINVAL, "bad window %d", window);

@@ -29,7 +29,8 @@ EXPORTED = (
     "dsi_model_create", "dsi_model_set_tensor", "dsi_model_destroy", "dsi_kv_create",
     "dsi_kv_destroy", "dsi_prefill", "dsi_verify", "dsi_verify_tree", "dsi_draft", "dsi_accept",
     "dsi_accept_noalloc", "dsi_kv_bytes", "dsi_kv_wrap", "dsi_kv_fork", "dsi_attend", "dsi_logprobs_workspace",
-    "dsi_logprobs", "dsi_kv_rollback", "dsi_kv_poison", "dsi_kv_length", "dsi_sync", "dsi_kv_export", "dsi_kv_import", "dsi_kv_set_length",
+    "dsi_logprobs", "dsi_rope_table", "dsi_rotate", "dsi_page_append", "dsi_page_attend_workspace", "dsi_page_attend",
+    "dsi_adjust", "dsi_kv_rollback", "dsi_kv_poison", "dsi_kv_length", "dsi_sync", "dsi_kv_export", "dsi_kv_import", "dsi_kv_set_length",
     "dsi_profile_begin", "dsi_profile_end", "dsi_profile_kernel", "dsi_profile_stream", "dsi_last_error",
 )
 DSI_K_QKV, DSI_K_ATTN, DSI_K_OPROJ, DSI_K_GATEUP, DSI_K_DOWN, DSI_K_HEAD, DSI_K_VERIFY = range(1, 8)
@@ -85,6 +86,70 @@ class dsi_logprobs_args(ctypes.Structure):
     ]
 
 
+DSI_ROPE_HALF, DSI_ROPE_PAIRS = 0, 1
+DSI_ROPE_PLAIN, DSI_ROPE_LINEAR, DSI_ROPE_BASE, DSI_ROPE_BANDS, DSI_ROPE_RAMP = range(5)
+
+
+class dsi_rope_spec(ctypes.Structure):
+    _fields_ = [
+        ("dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+        ("low", ctypes.c_double), ("high", ctypes.c_double), ("context", ctypes.c_double),
+    ]
+
+
+class dsi_rope(ctypes.Structure):
+    _fields_ = [
+        ("style", ctypes.c_int32), ("dim", ctypes.c_int32), ("d_freq", ctypes.c_void_p), ("gain", ctypes.c_float),
+    ]
+
+
+class dsi_rotate_args(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("ld_q", ctypes.c_int64), ("ld_k", ctypes.c_int64),
+        ("ld_q_out", ctypes.c_int64), ("ld_k_out", ctypes.c_int64), ("d_q", ctypes.c_void_p), ("d_k", ctypes.c_void_p),
+        ("d_pos", ctypes.c_void_p), ("d_gain_q", ctypes.c_void_p), ("d_gain_k", ctypes.c_void_p),
+        ("eps", ctypes.c_float), ("rope", dsi_rope), ("d_q_out", ctypes.c_void_p), ("d_k_out", ctypes.c_void_p),
+    ]
+
+
+class dsi_pages(ctypes.Structure):
+    _fields_ = [
+        ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("kvdtype", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
+        ("n_windows", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("d_table", ctypes.c_void_p),
+        ("d_len", ctypes.c_void_p), ("d_row0", ctypes.c_void_p),
+    ]
+
+
+class dsi_page_append_args(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("dtype", ctypes.c_int32), ("ld_q", ctypes.c_int64),
+        ("ld_k", ctypes.c_int64), ("ld_v", ctypes.c_int64), ("ld_q_out", ctypes.c_int64), ("d_q", ctypes.c_void_p),
+        ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("d_pos", ctypes.c_void_p), ("d_gain_q", ctypes.c_void_p),
+        ("d_gain_k", ctypes.c_void_p), ("eps", ctypes.c_float), ("rope", dsi_rope), ("d_q_out", ctypes.c_void_p),
+    ]
+
+
+class dsi_page_attend_args(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("dtype", ctypes.c_int32), ("reach", ctypes.c_int32),
+        ("ld_q", ctypes.c_int64), ("ld_out", ctypes.c_int64), ("d_q", ctypes.c_void_p), ("scale", ctypes.c_float),
+        ("d_out", ctypes.c_void_p), ("d_ws", ctypes.c_void_p), ("ws_bytes", ctypes.c_size_t),
+    ]
+
+
+class dsi_adjust_args(ctypes.Structure):
+    _fields_ = [
+        ("n_windows", ctypes.c_int32), ("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("n_bias", ctypes.c_int32), ("ld", ctypes.c_int64), ("ld_out", ctypes.c_int64), ("ld_seen", ctypes.c_int64),
+        ("ld_allowed", ctypes.c_int64), ("d_logits", ctypes.c_void_p), ("d_seen", ctypes.c_void_p),
+        ("d_n_seen", ctypes.c_void_p), ("d_tokens", ctypes.c_void_p), ("d_repetition", ctypes.c_void_p),
+        ("d_frequency", ctypes.c_void_p), ("d_presence", ctypes.c_void_p), ("d_bias_ids", ctypes.c_void_p),
+        ("d_bias", ctypes.c_void_p), ("d_allowed", ctypes.c_void_p), ("d_out", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -116,6 +181,12 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "dsi_attend": ([P, P, ctypes.POINTER(dsi_attend_args)], I32),
         "dsi_logprobs_workspace": ([I32, I32, I32, ctypes.POINTER(SZ)], I32),
         "dsi_logprobs": ([P, ctypes.POINTER(dsi_logprobs_args)], I32),
+        "dsi_rope_table": ([ctypes.POINTER(dsi_rope_spec), ctypes.POINTER(ctypes.c_double), ctypes.POINTER(F)], I32),
+        "dsi_rotate": ([P, ctypes.POINTER(dsi_rotate_args)], I32),
+        "dsi_page_append": ([P, ctypes.POINTER(dsi_pages), ctypes.POINTER(dsi_page_append_args)], I32),
+        "dsi_page_attend_workspace": ([ctypes.POINTER(dsi_pages), I32, I32, ctypes.POINTER(SZ)], I32),
+        "dsi_page_attend": ([P, ctypes.POINTER(dsi_pages), ctypes.POINTER(dsi_page_attend_args)], I32),
+        "dsi_adjust": ([P, ctypes.POINTER(dsi_adjust_args)], I32),
         "dsi_kv_rollback": ([P, I32, I32], I32),
         "dsi_kv_poison": ([P, I32], I32),
         "dsi_kv_length": ([P, I32, ctypes.POINTER(ctypes.c_int32)], I32),
@@ -258,6 +329,73 @@ def dsi_logprobs(stream: int, rows: int, vocab: int, d_logits, d_targets, n_top:
     a = dsi_logprobs_args(rows, vocab, dtype, n_top, ld or vocab, _ptr(d_logits), _ptr(d_targets), temperature,
                           _ptr(d_logprob), _ptr(d_entropy), _ptr(d_top_ids), _ptr(d_top_logprobs), _ptr(d_ws), ws_bytes)
     _check(load().dsi_logprobs(stream or None, ctypes.byref(a)))
+
+
+def make_rope(dim: int, d_freq, gain: float = 1.0, style: int = DSI_ROPE_HALF) -> dsi_rope:
+    return dsi_rope(style, dim, _ptr(d_freq), gain)
+
+
+def dsi_rope_table(dim: int, base: float = 10000.0, scaling: int = DSI_ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
+                   high: float = 32.0, context: float = 0.0):
+    """Returns (radians per position of each rotated pair, as a list; gain)."""
+    freq, gain = (ctypes.c_double * max(1, dim // 2))(), ctypes.c_float()
+    spec = dsi_rope_spec(dim, scaling, base, factor, low, high, context)
+    _check(load().dsi_rope_table(ctypes.byref(spec), freq, ctypes.byref(gain)))
+    return list(freq), gain.value
+
+
+def dsi_rotate(stream: int, rows: int, n_heads: int, n_kv_heads: int, head_dim: int, d_q, d_k, d_pos, d_q_out, d_k_out,
+               rope: dsi_rope, dtype: int = DSI_F32, ld_q: int = 0, ld_k: int = 0, ld_q_out: int = 0, ld_k_out: int = 0,
+               d_gain_q=None, d_gain_k=None, eps: float = 1e-5):
+    """ld_*: entries from one row to the next (0: its heads and nothing else)."""
+    nq, nk = n_heads * head_dim, n_kv_heads * head_dim
+    a = dsi_rotate_args(rows, n_heads, n_kv_heads, head_dim, dtype, ld_q or nq, ld_k or nk, ld_q_out or nq, ld_k_out or nk,
+                        _ptr(d_q), _ptr(d_k), _ptr(d_pos), _ptr(d_gain_q), _ptr(d_gain_k), eps, rope, _ptr(d_q_out),
+                        _ptr(d_k_out))
+    _check(load().dsi_rotate(stream or None, ctypes.byref(a)))
+
+
+def make_pages(n_kv_heads: int, head_dim: int, kvdtype: int, n_pages: int, page_size: int, d_k, d_v, n_windows: int,
+               max_pages: int, d_table, d_len, d_row0) -> dsi_pages:
+    """The tensors must live as long as calls use what is returned."""
+    return dsi_pages(n_kv_heads, head_dim, kvdtype, n_pages, page_size, _ptr(d_k), _ptr(d_v), n_windows, max_pages,
+                     _ptr(d_table), _ptr(d_len), _ptr(d_row0))
+
+
+def dsi_page_append(stream: int, pages: dsi_pages, rows: int, n_heads: int, d_q, d_k, d_v, d_q_out, rope: dsi_rope,
+                    dtype: int = DSI_F32, ld_q: int = 0, ld_k: int = 0, ld_v: int = 0, ld_q_out: int = 0, d_pos=None,
+                    d_gain_q=None, d_gain_k=None, eps: float = 1e-5):
+    nq, nk = n_heads * pages.head_dim, pages.n_kv_heads * pages.head_dim
+    a = dsi_page_append_args(rows, n_heads, dtype, ld_q or nq, ld_k or nk, ld_v or nk, ld_q_out or nq, _ptr(d_q), _ptr(d_k),
+                             _ptr(d_v), _ptr(d_pos), _ptr(d_gain_q), _ptr(d_gain_k), eps, rope, _ptr(d_q_out))
+    _check(load().dsi_page_append(stream or None, ctypes.byref(pages), ctypes.byref(a)))
+
+
+def dsi_page_attend_workspace(pages: dsi_pages, rows: int, n_heads: int) -> int:
+    """Bytes of the workspace that dsi_page_attend needs for these sizes."""
+    out = ctypes.c_size_t()
+    _check(load().dsi_page_attend_workspace(ctypes.byref(pages), rows, n_heads, ctypes.byref(out)))
+    return out.value
+
+
+def dsi_page_attend(stream: int, pages: dsi_pages, rows: int, n_heads: int, d_q, d_out, d_ws, ws_bytes: int,
+                    dtype: int = DSI_F32, reach: int = 0, ld_q: int = 0, ld_out: int = 0, scale: float = 0.0):
+    n = n_heads * pages.head_dim
+    a = dsi_page_attend_args(rows, n_heads, dtype, reach, ld_q or n, ld_out or n, _ptr(d_q), scale, _ptr(d_out), _ptr(d_ws),
+                             ws_bytes)
+    _check(load().dsi_page_attend(stream or None, ctypes.byref(pages), ctypes.byref(a)))
+
+
+def dsi_adjust(stream: int, n_windows: int, rows: int, vocab: int, d_logits, d_out, dtype: int = DSI_F32, ld: int = 0,
+               ld_out: int = 0, d_seen=None, d_n_seen=None, ld_seen: int = 0, d_tokens=None, d_repetition=None,
+               d_frequency=None, d_presence=None, n_bias: int = 0, d_bias_ids=None, d_bias=None, d_allowed=None,
+               ld_allowed: int = 0):
+    """ld, ld_out: 0: vocab; ld_allowed: 0: (vocab + 31) // 32 words."""
+    a = dsi_adjust_args(n_windows, rows, vocab, dtype, n_bias, ld or vocab, ld_out or vocab, ld_seen,
+                        ld_allowed or (vocab + 31) // 32, _ptr(d_logits), _ptr(d_seen), _ptr(d_n_seen), _ptr(d_tokens),
+                        _ptr(d_repetition), _ptr(d_frequency), _ptr(d_presence), _ptr(d_bias_ids) if n_bias else None,
+                        _ptr(d_bias) if n_bias else None, _ptr(d_allowed), _ptr(d_out))
+    _check(load().dsi_adjust(stream or None, ctypes.byref(a)))
 
 
 def dsi_kv_rollback(kv: int, window: int, new_len: int):

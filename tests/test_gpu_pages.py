@@ -1,0 +1,202 @@
+"""dsi_page_attend on the GPU against softmax(scale q K^T) V in 64 bits: types,
+head layouts, pages, lengths, reach, and what must not be read."""
+import math
+
+import pytest
+import torch
+
+from page_cases import HALF_STEP, KIND, Step, attend64
+from paper_2405_14105_amd import dsi
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def attend(step, q, hq, scale=0.0, pages=None, stream=None, out=None, reach=None):
+    """q [n][hq * hd]; outputs start at 7."""
+    out = torch.full_like(q, 7.0) if out is None else out
+    pages = pages or step.pages()
+    n = dsi.dsi_page_attend_workspace(pages, step.n, hq)
+    ws = torch.full((n + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    s = stream or torch.cuda.current_stream()
+    dsi.dsi_page_attend(s.cuda_stream, pages, step.n, hq, q, out, ws, n, KIND[q.dtype], step.reach if reach is None else reach, q.stride(0), out.stride(0), scale)
+    torch.cuda.synchronize()
+    assert (ws[n:] == 0xA5).all()
+    return out
+
+
+def tolerance(step, ref, mass, big, act):
+    """A score sums hd products of up to three parts each in fp32: at most hd / 16 * 3 + 4 additions after
+    each other, 2^-24 of the sum of magnitudes `big` each; its exponent and exp2 add 4 2^-24 (1 + big).  A
+    probability is off by that relatively, and so is its share of the sum: twice.  The outputs sum len / 16 steps."""
+    n = max(p + r for p, r in zip(step.past, step.rows))
+    tol = mass * ((2 * (step.hd // 16 * 3 + 8) * (1 + big) + n / 16 + 16) * 2.0 ** -24)
+    if act == BF16:
+        # the output's rounding, and a probability's where there are many rows (numerator; the sum is of unrounded ones)
+        tol = tol + ref.abs() * HALF_STEP[BF16] + mass * HALF_STEP[BF16]
+    return tol
+
+
+def check(step, hq, act, scale=0.0, seed=5, ld=0):
+    q = (torch.randn((step.n, ld or hq * step.hd), generator=torch.Generator().manual_seed(seed)) * 2).to(act)
+    ref, mass, big = attend64(step, q[:, :hq * step.hd].view(step.n, hq, step.hd), hq, scale)
+    step.to("cuda")
+    qd = q.cuda()
+    got = attend(step, qd[:, :hq * step.hd], hq, scale).cpu().view(step.n, hq, step.hd)
+    live = slice(step.before, step.before + sum(step.rows))
+    assert (got[:live.start] == 7).all() and (got[live.stop:] == 7).all()
+    err = (got[live].double() - ref[live]).abs()
+    tol = tolerance(step, ref, mass, big, act)[live]
+    assert torch.isfinite(got[live]).all() and (err <= tol).all(), ((err / tol).max(), err.max())
+    return got
+
+
+@pytest.mark.parametrize("hd", [32, 64, 96, 128])
+@pytest.mark.parametrize("kv", [F32, BF16])
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_types_and_head_dims(hd, kv, act):
+    check(Step([1, 5, 3], [70, 0, 130], 2, hd, kv, 32, seed=hd), 6, act)
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (4, 4), (8, 2), (5, 1), (33, 1), (80, 2)])
+def test_head_groups(hq, hkv):
+    check(Step([2, 7], [40, 97], hkv, 64, BF16, 64), hq, F32)
+
+
+@pytest.mark.parametrize("page", [32, 96, 256])
+@pytest.mark.parametrize("past", [[0, 1, 31], [32, 33, 63], [64, 127, 128], [255, 256, 257], [1000, 5, 700]])
+def test_lengths_and_pages(page, past):
+    check(Step([1, 2, 34], past, 2, 64, BF16, page, seed=past[0]), 4, BF16)
+
+
+@pytest.mark.parametrize("rows", [[0, 0, 3, 0], [1], [17, 0, 16], [65, 1], [129], [300, 2, 1]])
+def test_rows(rows):
+    check(Step(rows, [50 * (b + 1) for b in range(len(rows))], 2, 32, BF16, 64, seed=len(rows), before=3, behind=4), 6, F32)
+
+
+@pytest.mark.parametrize("reach", [1, 2, 31, 32, 33, 100, 5000])
+@pytest.mark.parametrize("kv", [F32, BF16])
+def test_reach(reach, kv):
+    """Pages before every row's reach are not in the table, positions before it are NaN."""
+    check(Step([3, 70, 1], [200, 333, 900], 2, 64, kv, 32, reach=reach, seed=reach), 4, F32)
+
+
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_long_contexts_are_cut_and_joined(act):
+    check(Step([1, 4, 2], [9000, 17, 4321], 1, 64, BF16, 64), 4, act)
+
+
+def test_strides_and_scale():
+    step = Step([4, 9], [33, 100], 2, 64, BF16, 32)
+    check(step, 4, F32, scale=0.5, ld=4 * 64 + 64)
+    check(Step([4, 9], [33, 100], 2, 64, BF16, 32), 4, BF16, scale=0.03, ld=4 * 64 + 8)
+
+
+def test_many_windows():
+    B = 150
+    g = torch.Generator().manual_seed(3)
+    rows = torch.randint(0, 3, (B,), generator=g).tolist()
+    past = torch.randint(0, 200, (B,), generator=g).tolist()
+    check(Step(rows, past, 1, 32, BF16, 32), 4, F32)
+
+
+@pytest.mark.parametrize("act,kv", [(F32, F32), (F32, BF16), (BF16, BF16)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("rows", [6, 90])
+def test_not_finite_values_reach_only_rows_that_see_them(act, kv, bad, rows):
+    """A key or value of a later row of the step, and of a row behind the reach."""
+    hq, reach = 4, 50
+    for what, at in (("k", 82), ("v", 82), ("v", 20), ("k", 20)):
+        step = Step([rows], [80], 2, 64, kv, 32, reach=reach)
+        q = torch.randn((step.n, hq, 64), generator=torch.Generator().manual_seed(1)).to(act)
+        clean, mass, big = attend64(step, q, hq)
+        page, place = int(step.table[0, at // 32]), at % 32
+        if page < 0:
+            continue
+        if what == "k":
+            step.k[page, 1, 0, 1, place, 7] = bad
+        else:
+            step.v[page, 1, 0, 9, place] = bad
+        step.to("cuda")
+        got = attend(step, q.view(step.n, -1).cuda(), hq).cpu().view(step.n, hq, 64).double()
+        pos = 80 + torch.arange(step.n)
+        sees = (at <= pos) & (at > pos - reach)
+        hit = torch.zeros_like(got, dtype=torch.bool)
+        if what == "k":
+            hit[:, 2:] = sees[:, None, None]
+        else:
+            hit[:, 2:, 9] = sees[:, None]
+        err = (got - clean).abs()
+        assert (err[~hit] <= tolerance(step, clean, mass, big, act)[~hit]).all(), (what, at)
+        if what == "v" or math.isnan(bad):
+            assert not torch.isfinite(got[hit]).any(), (what, at)
+
+
+def test_what_does_not_fit_gives_nan():
+    """Windows with a negative length, with rows past the table, with a bad page; the others are right."""
+    hq = 4
+    step = Step([3, 2, 4, 2, 40], [100, 40, 64, 10, 200], 2, 64, BF16, 32)
+    q = torch.randn((step.n, hq, 64), generator=torch.Generator().manual_seed(1))
+    ref, mass, big = attend64(step, q, hq)
+    step.table[0, 1] = step.k.shape[0]      # a page behind the pool: every row sees it
+    step.table[2, 2] = -1                   # every row of window 2 sees position 64 on
+    step.len[1] = -1
+    step.table[4, 7] = 1 << 30              # positions 224 ..: rows from 24 on see them
+    step.to("cuda")
+    got = attend(step, q.view(step.n, -1).cuda(), hq).cpu().view(step.n, hq, 64)
+    nan = torch.zeros(step.n, dtype=torch.bool)
+    nan[:9] = True
+    nan[11 + 24:] = True
+    assert got[nan].isnan().all()
+    assert ((got.double() - ref).abs() <= tolerance(step, ref, mass, big, F32))[~nan].all()
+    step.len[:] = torch.tensor([100, 2 ** 31 - 1, 64, step.most * 32 - 1, 200])
+    got = attend(step, q.view(step.n, -1).cuda(), hq).cpu().view(step.n, hq, 64)
+    assert got[3:5].isnan().all() and got[9:11].isnan().all() and torch.isfinite(got[11:35]).all()
+
+
+def test_rows_of_windows_that_are_out_of_order_stay_in_bounds():
+    step = Step([3, 5], [100, 40], 2, 64, BF16, 32).to("cuda")
+    step.row0 = torch.tensor([-5, 20, 3], dtype=torch.int32, device="cuda")
+    attend(step, torch.randn((step.n, 256), device="cuda"), 4)
+    step.row0 = torch.tensor([2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    attend(step, torch.randn((step.n, 256), device="cuda"), 4)
+
+
+def test_one_call_gives_the_same_bits():
+    step = Step([1, 4, 70], [3000, 17, 500], 2, 128, BF16, 64).to("cuda")
+    q = torch.randn((step.n, 8 * 128), device="cuda")
+    first = attend(step, q, 8)
+    for _ in range(3):
+        assert torch.equal(attend(step, q, 8), first)
+
+
+def test_windows_may_share_pages():
+    step = Step([2, 2], [96, 96], 2, 64, BF16, 32)
+    step.K[1][:96], step.V[1][:96] = step.K[0][:96], step.V[0][:96]
+    step.table[1, :3] = step.table[0, :3]
+    check(step, 4, F32)
+
+
+def test_captured_and_replayed_with_other_lengths():
+    """A graph reads lengths, tables and rows when it runs; eager calls go on between replays."""
+    hq, B = 4, 3
+    step = Step([4, 4, 4], [300, 10, 4000], 2, 64, BF16, 64).to("cuda")
+    q = torch.randn((step.n, hq * 64), device="cuda")
+    out = torch.zeros_like(q)
+    pages = step.pages()
+    n = dsi.dsi_page_attend_workspace(pages, step.n, hq)
+    ws = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        dsi.dsi_page_attend(torch.cuda.current_stream().cuda_stream, pages, step.n, hq, q, out, ws, n)
+    for lens, row0 in (([300, 10, 4000], [0, 4, 8, 12]), ([20, 0, 1000], [0, 1, 1, 12]), ([0, 10, 3999], [0, 4, 11, 12]), ([300, 10, 4000], [0, 4, 8, 12])):
+        step.len.copy_(torch.tensor(lens))
+        step.row0.copy_(torch.tensor(row0))
+        q.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        # bits: rows that see positions the pool does not hold are NaN both times
+        assert torch.equal(out.view(torch.int32), attend(step, q, hq, pages=pages).view(torch.int32))
