@@ -519,21 +519,26 @@ hipError_t launch_rotate(RotateArgs a, bool wide, hipStream_t s);
 // Attention of a step's rows over pages (pages.hip)
 struct PageAttnArgs {
   PageArgs pg;
-  int rows, nq, bf16, reach;   // bf16: queries and outputs
+  int rows, nq, G, bf16;   // G = nq / nkv; bf16: queries and outputs
+  int reach;            // 0: all
   size_t ldq, ldo;
   const void* q;
   void* out;
   float scale2;         // scale * log2 e
-  // one class of windows: those with qlo..qhi queries of a KV head
+};
+// one class of windows: those with qlo..qhi queries of a KV head
+struct PageClass {
   int qlo, qhi;
-  int tile;             // queries per tile
-  int target;           // items (of all KV heads) a launch is cut into where its windows are long
-  int least;            // units of keys an item has at least
-  float* part;          // [slots][head_dim][tile]
-  float2* ml;           // [slots][tile]: maximum (base 2) and sum
+  int qw;               // 32 queries of a tile (0: one or two, as the window has queries)
+  // items * qw that a call is cut into where its windows are long: `once` of them as
+  // long as an item then has no more than `enough` units of keys, up to `most`
+  int once, most, enough;
+  double inv_once, inv_most;
+  float* part;          // [slots][32][head_dim]
+  float2* ml;           // [slots][32]: maximum (base 2) and sum
 };
 size_t page_attend_workspace_bytes(const PageArgs& pg, int rows, int nq);
-hipError_t launch_page_attend(PageAttnArgs a, void* ws, hipStream_t s);
+hipError_t launch_page_attend(const PageAttnArgs& a, void* ws, hipStream_t s);
 
 // Penalties, biases and masks on rows of logits (adjust.hip)
 struct AdjustArgs {

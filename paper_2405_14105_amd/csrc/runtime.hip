@@ -2360,7 +2360,9 @@ dsi_status dsi_page_attend(void* stream, const dsi_pages* pages, const dsi_page_
   d.rows = a->rows;
   d.nq = a->n_heads;
   d.bf16 = a->dtype == DSI_BF16;
-  d.reach = a->reach;
+  // a reach beyond the table sees all there is
+  d.reach = (long long)a->reach < (long long)pages->max_pages * pages->page_size ? a->reach : 0;
+  d.G = a->n_heads / pages->n_kv_heads;
   d.ldq = (size_t)a->ld_q;
   d.ldo = (size_t)a->ld_out;
   d.q = a->d_q;

@@ -59,15 +59,26 @@ def test_types_and_head_dims(hd, kv, act):
     check(Step([1, 5, 3], [70, 0, 130], 2, hd, kv, 32, seed=hd), 6, act)
 
 
+@pytest.mark.parametrize("hd", [32, 64, 96, 128])
+@pytest.mark.parametrize("kv", [F32, BF16])
+@pytest.mark.parametrize("act", [F32, BF16])
+@pytest.mark.parametrize("rows,past", [([100, 2, 0, 30], [70, 5, 9, 300]), ([97], [0]), ([200], [133])])
+def test_types_and_head_dims_of_many_rows(hd, kv, act, rows, past):
+    """Windows of many rows, alone and beside windows of few."""
+    check(Step(rows, past, 2, hd, kv, 32, seed=hd, behind=3), 6, act)
+
+
 @pytest.mark.parametrize("hq,hkv", [(1, 1), (4, 4), (8, 2), (5, 1), (33, 1), (80, 2)])
-def test_head_groups(hq, hkv):
-    check(Step([2, 7], [40, 97], hkv, 64, BF16, 64), hq, F32)
+@pytest.mark.parametrize("rows", [[2, 7], [2, 70]])
+def test_head_groups(hq, hkv, rows):
+    check(Step(rows, [40, 97], hkv, 64, BF16, 64), hq, F32)
 
 
 @pytest.mark.parametrize("page", [32, 96, 256])
 @pytest.mark.parametrize("past", [[0, 1, 31], [32, 33, 63], [64, 127, 128], [255, 256, 257], [1000, 5, 700]])
 def test_lengths_and_pages(page, past):
     check(Step([1, 2, 34], past, 2, 64, BF16, page, seed=past[0]), 4, BF16)
+    check(Step([1, 2, 134], past, 2, 64, BF16, page, seed=past[0]), 4, BF16)
 
 
 @pytest.mark.parametrize("rows", [[0, 0, 3, 0], [1], [17, 0, 16], [65, 1], [129], [300, 2, 1]])
@@ -80,11 +91,13 @@ def test_rows(rows):
 def test_reach(reach, kv):
     """Pages before every row's reach are not in the table, positions before it are NaN."""
     check(Step([3, 70, 1], [200, 333, 900], 2, 64, kv, 32, reach=reach, seed=reach), 4, F32)
+    check(Step([3, 170, 1], [200, 333, 900], 2, 64, kv, 32, reach=reach, seed=reach), 4, F32)
 
 
 @pytest.mark.parametrize("act", [F32, BF16])
 def test_long_contexts_are_cut_and_joined(act):
     check(Step([1, 4, 2], [9000, 17, 4321], 1, 64, BF16, 64), 4, act)
+    check(Step([1, 4, 120], [9000, 17, 4321], 1, 64, BF16, 64), 4, act)
 
 
 def test_strides_and_scale():
@@ -103,7 +116,7 @@ def test_many_windows():
 
 @pytest.mark.parametrize("act,kv", [(F32, F32), (F32, BF16), (BF16, BF16)])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-@pytest.mark.parametrize("rows", [6, 90])
+@pytest.mark.parametrize("rows", [6, 90, 150])
 def test_not_finite_values_reach_only_rows_that_see_them(act, kv, bad, rows):
     """A key or value of a later row of the step, and of a row behind the reach."""
     hq, reach = 4, 50
@@ -133,9 +146,9 @@ def test_not_finite_values_reach_only_rows_that_see_them(act, kv, bad, rows):
             assert not torch.isfinite(got[hit]).any(), (what, at)
 
 
-def test_what_does_not_fit_gives_nan():
+@pytest.mark.parametrize("hq", [4, 12])
+def test_what_does_not_fit_gives_nan(hq):
     """Windows with a negative length, with rows past the table, with a bad page; the others are right."""
-    hq = 4
     step = Step([3, 2, 4, 2, 40], [100, 40, 64, 10, 200], 2, 64, BF16, 32)
     q = torch.randn((step.n, hq, 64), generator=torch.Generator().manual_seed(1))
     ref, mass, big = attend64(step, q, hq)
@@ -159,12 +172,14 @@ def test_rows_of_windows_that_are_out_of_order_stay_in_bounds():
     step = Step([3, 5], [100, 40], 2, 64, BF16, 32).to("cuda")
     step.row0 = torch.tensor([-5, 20, 3], dtype=torch.int32, device="cuda")
     attend(step, torch.randn((step.n, 256), device="cuda"), 4)
+    attend(step, torch.randn((step.n, 4096), device="cuda"), 64)
     step.row0 = torch.tensor([2 ** 31 - 1, -2 ** 31, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
     attend(step, torch.randn((step.n, 256), device="cuda"), 4)
 
 
-def test_one_call_gives_the_same_bits():
-    step = Step([1, 4, 70], [3000, 17, 500], 2, 128, BF16, 64).to("cuda")
+@pytest.mark.parametrize("rows", [[1, 4, 40], [1, 4, 170]])
+def test_one_call_gives_the_same_bits(rows):
+    step = Step(rows, [3000, 17, 500], 2, 128, BF16, 64).to("cuda")
     q = torch.randn((step.n, 8 * 128), device="cuda")
     first = attend(step, q, 8)
     for _ in range(3):
