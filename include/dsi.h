@@ -460,8 +460,7 @@ typedef struct {
  *                  sqrt(mean(x^2) + eps) over its head and multiplied by the gain
  *   d_q_out, d_k_out   [rows][ld_q_out], [rows][ld_k_out].  In place (the same
  *                  pointer and stride) or apart from the input
- * No alignment beyond the type's; 16-byte aligned pointers and strides, and a
- * rope.dim that is a multiple of 16, are faster.  rows = 0 does nothing. */
+ * No alignment beyond the type's.  rows = 0 does nothing. */
 typedef struct {
   int32_t rows, n_heads, n_kv_heads, head_dim, dtype;
   int64_t ld_q, ld_k, ld_q_out, ld_k_out;

@@ -21,6 +21,9 @@ namespace {
 
 constexpr int kAdjThreads = 256;
 constexpr int kAdjChunk = 4096;
+// workgroups up to which a window's rows are spread (7 x 6 x 128256, 2048 tokens seen:
+// 16.0 us with 256, 13.5 with 512 or 1024; 16 x 4 in bf16: 15.8, 16.0, 12.6, with 2048 14.0)
+constexpr int kAdjFull = 1024;
 static_assert(kMaxBias < 1 << 11 && kMaxCount == 1 << 21, "a word holds both");
 
 // 16 bytes of a row, whose alignment is the type's (T holds bit patterns:
@@ -75,14 +78,18 @@ __global__ __launch_bounds__(kAdjThreads) void k_adjust(AdjustArgs a) {
   const int i0 = g * a.rpg, i1 = min(i0 + a.rpg, a.R);
   auto row_of = [&](int i) { return (const T*)a.z + ((size_t)b * a.R + i) * a.ld; };
   u32x4 z[PER];
+  uint32_t ok[PER];   // the mask's bits, of a run's entries the lowest
   auto load_row = [&](int i) {
+    const uint32_t* mask = a.allowed ? a.allowed + ((size_t)b * a.R + i) * a.lda : nullptr;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const int v = v0 + (j * kAdjThreads + tid) * N;
-      if (v < a.V) z[j] = load_run(row_of(i), v, a.V);
+      if (v >= a.V) continue;
+      if constexpr (!PLACE) z[j] = load_run(row_of(i), v, a.V);
+      ok[j] = mask ? mask[v >> 5] >> (v & 31) : ~0u;
     }
   };
-  if constexpr (!PLACE) load_row(i0);
+  load_row(i0);
   for (int j = tid; j < kAdjChunk / 4; j += kAdjThreads) ((u32x4*)word)[j] = u32x4{0, 0, 0, 0};
   __syncthreads();
   for (int j = tid; j < a.n_bias; j += kAdjThreads) {
@@ -97,7 +104,15 @@ __global__ __launch_bounds__(kAdjThreads) void k_adjust(AdjustArgs a) {
   if (a.seen) {
     const int* s = a.seen + (size_t)b * a.ldseen;
     const int n = min(max(a.n_seen[b], 0), (int)a.ldseen);
-    for (int j = tid; j < n; j += kAdjThreads) count(s[j]);
+    // eight loads of a thread in flight (one after the other they were half the time
+    // of 7 windows x 6 rows x 128256 with 2048 tokens seen)
+    for (int j0 = tid; j0 < n; j0 += 8 * kAdjThreads) {
+      int tok[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) tok[k] = j0 + k * kAdjThreads < n ? s[j0 + k * kAdjThreads] : -1;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) count(tok[k]);
+    }
   }
   const int* own = a.tokens ? a.tokens + (size_t)b * a.R : nullptr;
   if (own)
@@ -110,7 +125,6 @@ __global__ __launch_bounds__(kAdjThreads) void k_adjust(AdjustArgs a) {
     if (own && tid == 0) count(own[i]);
     __syncthreads();
     T* out = (T*)a.out + ((size_t)b * a.R + i) * a.ldo;
-    const uint32_t* mask = a.allowed ? a.allowed + ((size_t)b * a.R + i) * a.lda : nullptr;
     u32x4 y[PER];
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -119,8 +133,7 @@ __global__ __launch_bounds__(kAdjThreads) void k_adjust(AdjustArgs a) {
       uint32_t w[N], any = 0;
 #pragma unroll
       for (int e = 0; e < N; ++e) any |= w[e] = word[at + e];
-      const uint32_t ok = mask ? mask[v >> 5] >> (v & 31) : ~0u;
-      const bool all = (~ok & ((1u << N) - 1)) == 0;
+      const bool all = (~ok[j] & ((1u << N) - 1)) == 0;
       if (PLACE && !any && all) continue;
       const u32x4 x = PLACE ? load_run(row_of(i), v, a.V) : z[j];
       uint32_t o[N];
@@ -133,7 +146,7 @@ __global__ __launch_bounds__(kAdjThreads) void k_adjust(AdjustArgs a) {
           t = t - f * (float)n - p;
         }
         if (w[e] >> 21) t += bias[(w[e] >> 21) - 1];
-        if (!(ok >> e & 1)) t = -INFINITY;
+        if (!(ok[j] >> e & 1)) t = -INFINITY;
         o[e] = __float_as_uint(t);
       }
       if constexpr (sizeof(T) == 4) {
@@ -145,7 +158,7 @@ __global__ __launch_bounds__(kAdjThreads) void k_adjust(AdjustArgs a) {
       if constexpr (PLACE) store_run(out, v, a.V, y[j]);
     }
     if (i + 1 < i1) {
-      if constexpr (!PLACE) load_row(i + 1);
+      load_row(i + 1);
       __syncthreads();   // the words are read before the next row's token enters them
     }
     if constexpr (!PLACE) {
@@ -164,7 +177,7 @@ hipError_t launch_adjust(AdjustArgs a, hipStream_t s) {
   a.chunks = (a.V - 1) / kAdjChunk + 1;
   // rows of a window share what it has seen, where there is work for the card without them
   const long long each = (long long)a.chunks * a.B;
-  a.groups = (int)std::min((long long)a.R, (1024 + each - 1) / each);
+  a.groups = (int)std::min((long long)a.R, (kAdjFull + each - 1) / each);
   a.rpg = (a.R + a.groups - 1) / a.groups;
   a.groups = (a.R + a.rpg - 1) / a.rpg;
   const dim3 grid((unsigned)(each * a.groups)), block(kAdjThreads);

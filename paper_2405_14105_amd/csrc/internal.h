@@ -511,10 +511,11 @@ struct RotateArgs {
   void* qo;
   void* ko;             // unused with pages
   PageArgs pg;
-  int passes, ppw, wpr; // head groups of a row, a wave's, and waves per row
+  int lph;              // lanes per head, a power of two
+  int passes, parts;    // groups of 64 / lph heads of a row, and workgroups that share them
   int row_blocks;       // workgroups of queries and keys; the others take values
 };
-hipError_t launch_rotate(RotateArgs a, bool wide, hipStream_t s);
+hipError_t launch_rotate(RotateArgs a, hipStream_t s);
 
 // Attention of a step's rows over pages (pages.hip)
 struct PageAttnArgs {

@@ -4,13 +4,16 @@
 //   y = x / sqrt(mean(x^2) + eps) * gain  (optional, per head)
 //   (a', b') = g (a cos t - b sin t, b cos t + a sin t),  t = p f_j
 //
-// Bound by reading and writing the rows once.  A lane holds VEC turned pairs of
-// one head in two 16-byte pieces (half style: VEC entries at j and VEC at j +
-// dim/2; pairs: 2 VEC entries in a row), 64 / LPH heads a wave at a time, so the
-// sines of a row are made once a wave and serve all heads that it works on.
-// Angles: p f is formed in fp64 in turns and reduced there; what is left, at
-// most half a turn, is rounded to fp32 (2^-24 of it) and goes to sincospi.
-// Rows, strides or a dim that 16-byte pieces do not fit take VEC = 1.
+// Bound by reading and writing the rows once.  A wave takes a row, or some of its
+// heads where there are few rows.  A lane holds VEC turned pairs of one head in two
+// 16-byte pieces (half style: VEC entries from j and VEC from j + dim/2 on; pairs: 2
+// VEC entries in a row), 64 / LPH heads a wave at a time, the next two groups of them
+// on their way meanwhile; what is not turned lies in further lanes, 2 VEC entries
+// each.  Loads and stores of 16 bytes need no more than the type's alignment; where a
+// dim fills no whole pieces the last ones overlap.
+// A row's sines are made once a wave, one pair a lane, and the lanes read those of
+// their pairs from LDS.  p f is formed in fp64 in turns and reduced there; what is
+// left, at most half a turn, is rounded to fp32 (2^-24 of it) and goes to sincospi.
 // Values of a page lie [dim][32 positions]: 32 positions of a head are turned
 // over in LDS so that full runs of 8 positions leave as 16 bytes; a step of one
 // row writes 2 bytes into each dim's run, as the layout has it.
@@ -23,48 +26,116 @@ namespace dsi {
 namespace {
 
 constexpr int kRotWaves = 4;
+constexpr int kRotPairs = 64;   // of a head, at most
+constexpr int kRotFull = 4096;  // waves that rows are spread over, head by head, where they are few
 
-template <typename T, int VEC>
-__device__ __forceinline__ void load_piece(const T* p, float (&v)[VEC]) {
-  if constexpr (VEC == 1) {
-    if constexpr (sizeof(T) == 2) v[0] = bf_bits2f(*p);
-    else v[0] = *p;
-  } else {
-    const u32x4 x = *(const u32x4*)p;
+// 16 bytes with the type's alignment
+template <typename T>
+struct Piece;
+template <>
+struct Piece<float> {
+  static constexpr int N = 4;
+  typedef uint32_t vec __attribute__((ext_vector_type(4), aligned(4)));
+};
+template <>
+struct Piece<uint16_t> {
+  static constexpr int N = 8;
+  typedef uint32_t vec __attribute__((ext_vector_type(4), aligned(2)));
+};
+// n of a piece's N entries (the others 0), as bits
+template <typename T>
+__device__ __forceinline__ u32x4 load_piece(const T* p, int n) {
+  constexpr int N = Piece<T>::N;
+  if (n >= N) return *(const typename Piece<T>::vec*)p;
+  u32x4 x = u32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (i < n) {
+      if constexpr (sizeof(T) == 2) x[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+      else x[i] = __float_as_uint(p[i]);
+    }
+  return x;
+}
+template <typename T>
+__device__ __forceinline__ void floats_of(const u32x4& x, float (&v)[Piece<T>::N]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
     if constexpr (sizeof(T) == 2) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(x[i] << 16);
-        v[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
-      }
+      v[2 * i] = __uint_as_float(x[i] << 16);
+      v[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
     } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(x[i]);
+      v[i] = __uint_as_float(x[i]);
     }
   }
 }
-// VEC entries of a type known at run time; 16-byte aligned runs where VEC > 1
-template <int VEC>
-__device__ __forceinline__ void store_piece(void* base, size_t at, bool bf16, const float (&v)[VEC]) {
-  if constexpr (VEC == 1) {
-    if (bf16) ((uint16_t*)base)[at] = f2bf_bits(v[0]);
-    else ((float*)base)[at] = v[0];
+template <int N>
+__device__ __forceinline__ void scale_by(float (&v)[N], float f, const float* g, int n) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    float x[4];
+    floats_of<float>(load_piece<float>(g + i, n - i), x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[i + e] = v[i + e] * f * x[e];
+  }
+}
+// n of N entries to `at` of an array whose type is known at run time
+template <int N>
+__device__ __forceinline__ void store_piece(void* base, size_t at, bool bf16, int n, const float (&v)[N]) {
+  if (n < N) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (i >= n) continue;
+      if (bf16) ((uint16_t*)base)[at + i] = f2bf_bits(v[i]);
+      else ((float*)base)[at + i] = v[i];
+    }
   } else if (bf16) {
-    uint32_t w[VEC / 2];
+    uint32_t w[N / 2];
 #pragma unroll
-    for (int i = 0; i < VEC / 2; ++i) w[i] = f2bf_pair(v[2 * i], v[2 * i + 1]);
-    if constexpr (VEC == 8) *(u32x4*)((uint16_t*)base + at) = u32x4{w[0], w[1], w[2], w[3]};
-    else *(uint2*)((uint16_t*)base + at) = uint2{w[0], w[1]};
+    for (int i = 0; i < N / 2; ++i) w[i] = f2bf_pair(v[2 * i], v[2 * i + 1]);
+    typedef uint32_t two __attribute__((ext_vector_type(2), aligned(2)));
+    uint16_t* d = (uint16_t*)base + at;
+    if constexpr (N == 8) *(Piece<uint16_t>::vec*)d = u32x4{w[0], w[1], w[2], w[3]};
+    else *(two*)d = two{w[0], w[1]};
   } else {
+    float* d = (float*)base + at;
 #pragma unroll
-    for (int i = 0; i < VEC / 4; ++i)
-      *(f32x4*)((float*)base + at + 4 * i) = f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+    for (int i = 0; i < N / 4; ++i)
+      *(Piece<float>::vec*)(d + 4 * i) = u32x4{__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])};
+  }
+}
+// the same into a block of keys, [hd/32][32 positions][32]; `at` is the position's
+// entry of dim 0, d the piece's first dim
+template <int N>
+__device__ __forceinline__ void store_key(void* base, size_t at, int d, bool bf16, int n, const float (&v)[N]) {
+  if ((d & 31) + N <= 32) {
+    store_piece<N>(base, at + (size_t)(d >> 5) * 1024 + (d & 31), bf16, n, v);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {   // over two of the layout's runs of 32 dims
+    const size_t to = at + (size_t)((d + i) >> 5) * 1024 + ((d + i) & 31);
+    if (i >= n) continue;
+    if (bf16) ((uint16_t*)base)[to] = f2bf_bits(v[i]);
+    else ((float*)base)[to] = v[i];
   }
 }
 
+// the sum over groups of n lanes (a power of two), for all of them: lanes of a row of
+// 16 meet by DPP patterns, of which the mirrors do where a half's lanes are alike
+__device__ __forceinline__ float sum_of_group(float s, int n) {
+  if (n > 1) s += dpp_from<0xB1, 0xF>(s, s);
+  if (n > 2) s += dpp_from<0x4E, 0xF>(s, s);
+  if (n > 4) s += dpp_from<0x141, 0xF>(s, s);
+  if (n > 8) s += dpp_from<0x140, 0xF>(s, s);
+  if (n > 16) s += __shfl_xor(s, 16);
+  if (n > 32) s += __shfl_xor(s, 32);
+  return s;
+}
+
 // values of one block of 32 positions and KV head
-template <typename T, int VEC>
+template <typename T>
 __device__ __forceinline__ void append_values(const RotateArgs& a, uint32_t (&tile)[32][129], int item) {
+  constexpr int N = Piece<T>::N;
   const PageArgs& p = a.pg;
   const int kvh = item % p.nkv;
   int in = 0;
@@ -86,13 +157,13 @@ __device__ __forceinline__ void append_values(const RotateArgs& a, uint32_t (&ti
   const int lo = max(len - kb * 32, 0), hi = (int)min(32ll, (long long)len + (r1 - r0) - (long long)kb * 32);
   const int first = r0 + kb * 32 - len;   // the row of the block's position 0
   const T* src = (const T*)a.v + (size_t)kvh * a.hd;
-  const int ppr = a.hd / VEC;             // pieces per row
+  const int ppr = a.hd / N;               // pieces per row
   for (int i = threadIdx.x + lo * ppr; i < hi * ppr; i += kRotWaves * 64) {
-    const int pos = i / ppr, d = (i - pos * ppr) * VEC;
-    float v[VEC];
-    load_piece<T, VEC>(src + (size_t)(first + pos) * a.ldv + d, v);
+    const int pos = i / ppr, d = (i - pos * ppr) * N;
+    float v[N];
+    floats_of<T>(load_piece<T>(src + (size_t)(first + pos) * a.ldv + d, N), v);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) tile[pos][d + e] = p.kvb ? (uint32_t)f2bf_bits(v[e]) : __float_as_uint(v[e]);
+    for (int e = 0; e < N; ++e) tile[pos][d + e] = p.kvb ? (uint32_t)f2bf_bits(v[e]) : __float_as_uint(v[e]);
   }
   __syncthreads();
   const size_t base = (size_t)blk * 32 * a.hd;
@@ -121,130 +192,163 @@ __device__ __forceinline__ void append_values(const RotateArgs& a, uint32_t (&ti
   }
 }
 
-template <typename T, int VEC>
-__global__ __launch_bounds__(kRotWaves * 64) void k_rotate(RotateArgs a) {
-  __shared__ uint32_t tile[32][129];
+template <typename T>
+__global__ __launch_bounds__(kRotWaves * 64, 4) void k_rotate(RotateArgs a) {
+  constexpr int VEC = Piece<T>::N;
+  __shared__ union {
+    uint32_t tile[32][129];
+    float2 turn[kRotWaves][kRotPairs];
+  } sh;
   if ((int)blockIdx.x >= a.row_blocks) {
-    append_values<T, VEC>(a, tile, (int)blockIdx.x - a.row_blocks);
+    append_values<T>(a, sh.tile, (int)blockIdx.x - a.row_blocks);
     return;
   }
-  const int lane = threadIdx.x & 63;
-  const long long wave = (long long)blockIdx.x * kRotWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = (int)(wave / a.wpr), part = (int)(wave - (long long)r * a.wpr);
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const long long wave = (long long)blockIdx.x * kRotWaves + w;
+  const int r = (int)(wave / a.parts), part = (int)(wave - (long long)r * a.parts);
   if (r >= a.rows) return;
   const PageArgs& p = a.pg;
+  // where the lane's two pieces lie in a head.  A last unit that would not be whole
+  // starts earlier: its first dupx and dupy entries are another lane's too, which
+  // makes the same of them.  na and nb are less than VEC only where a head has no
+  // more pairs, or no more of what is not turned.
+  const int pairs = a.dim / 2, turned = (pairs + VEC - 1) / VEC;   // units with pairs
+  const int u = lane & (a.lph - 1), hpp = 64 / a.lph;
+  int pa, pb, na = VEC, nb = VEC, j0 = 0, over;
+  if (u < turned) {
+    j0 = max(min(u * VEC, pairs - VEC), 0);
+    over = u * VEC - j0;
+    const int n = min(VEC, pairs - j0);
+    if (a.style) {
+      pa = 2 * j0, pb = pa + VEC, na = min(VEC, 2 * n), nb = max(0, 2 * n - VEC);
+      over *= 2;
+    } else {
+      pa = j0, pb = pairs + j0, na = nb = n;
+    }
+  } else {
+    const int at = a.dim + (u - turned) * 2 * VEC, rest = a.hd - a.dim;
+    pa = rest >= 2 * VEC ? min(at, a.hd - 2 * VEC) : a.dim;
+    pb = rest >= VEC ? min(pa + VEC, a.hd - VEC) : a.hd;
+    na = at < a.hd ? min(VEC, rest) : 0;
+    nb = at < a.hd && rest > VEC ? VEC : 0;
+    over = at - pa + (pa + VEC - pb);
+  }
+  const bool split = u < turned && !a.style;   // both pieces overlap alike
+  const int dupx = split ? over : u < turned || a.hd - a.dim >= 2 * VEC ? min(over, VEC) : 0;
+  const int dupy = split ? over : u < turned || a.hd - a.dim >= 2 * VEC ? max(0, over - VEC) : over;
+  const int heads = a.nq + a.nk;
+  // the wave's groups of hpp heads
+  const int p0 = part * a.passes / a.parts, p1 = (part + 1) * a.passes / a.parts;
+  struct Raw {
+    u32x4 a, b;
+  };
+  auto load = [&](int ps) {
+    const int h = ps * hpp + lane / a.lph;
+    Raw x{u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}};
+    if (ps >= p1 || na <= 0 || h >= heads) return x;
+    const T* src = h < a.nq ? (const T*)a.q + (size_t)r * a.ldq + (size_t)h * a.hd : (const T*)a.k + (size_t)r * a.ldk + (size_t)(h - a.nq) * a.hd;
+    x.a = load_piece<T>(src + pa, na);
+    x.b = load_piece<T>(src + pb, nb);
+    return x;
+  };
+  Raw x0 = load(p0), x1 = load(p0 + 1);
   // the row's position, and where its keys go
-  int pos = a.pos && a.dim ? a.pos[r] : 0;
-  long long page_row = -1;   // block of KV head 0
-  int slot = 0;
+  int pos = a.pos && a.dim ? a.pos[r] : 0, slot = 0;
+  long long block = -1;   // of KV head 0
   if (p.n_windows) {
     const int b = window_of_row(p, a.rows, r);
     if (b < 0) return;
     const long long at = (long long)p.len[b] + (r - min(max(p.row0[b], 0), a.rows));
     if (!a.pos) pos = (int)at;
     if (p.len[b] >= 0 && at < window_positions(p)) {
-      page_row = block_of(p, b, 0, (int)(at >> 5));
+      block = block_of(p, b, 0, (int)(at >> 5));
       slot = (int)(at & 31);
     }
   }
-  const int units = a.hd / (2 * VEC);
-  int lph = 1;               // lanes per head: units, rounded up to a power of two
-  while (lph < units) lph *= 2;
-  const int u = lane & (lph - 1), hpp = 64 / lph;
-  const bool live = u < units;
-  // where the lane's two pieces lie in a head, and the pairs they make
-  const int turned = a.dim / (2 * VEC);     // units of whole turned pairs (half style)
-  int pa, pb;
-  if (a.style || u >= turned) pa = u * 2 * VEC, pb = pa + VEC;
-  else pa = u * VEC, pb = a.dim / 2 + u * VEC;
+  if (lane < pairs) {
+    const double t = (double)pos * a.freq[lane] * 0.15915494309189533577;   // turns
+    float s, c;
+    sincospif(2.f * (float)(t - rint(t)), &s, &c);
+    sh.turn[w][lane] = make_float2(c * a.gain, s * a.gain);
+  }
+  // the wave's own: the LDS takes a wave's accesses in their order
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   float cs[VEC], sn[VEC];
 #pragma unroll
   for (int e = 0; e < VEC; ++e) {
-    const int j = u * VEC + e;
-    cs[e] = 1.f;
-    sn[e] = 0.f;
-    if (live && j < a.dim / 2) {
-      const double t = (double)pos * a.freq[j] * 0.15915494309189533577;   // turns
-      sincospif(2.f * (float)(t - rint(t)), &sn[e], &cs[e]);
-      cs[e] *= a.gain;
-      sn[e] *= a.gain;
-    }
+    const float2 v = sh.turn[w][min(j0 + e, kRotPairs - 1)];
+    cs[e] = v.x;
+    sn[e] = v.y;
   }
-  const int heads = a.nq + a.nk;
-  const int p0 = part * a.ppw, p1 = min(p0 + a.ppw, a.passes);
   for (int ps = p0; ps < p1; ++ps) {
-    const int h = ps * hpp + lane / lph;
-    const bool on = live && h < heads, isq = h < a.nq;
+    const Raw raw = x0;
+    x0 = x1;
+    x1 = load(ps + 2);
+    const int h = ps * hpp + lane / a.lph;
+    const bool on = na > 0 && h < heads, isq = h < a.nq;
     const int hh = isq ? h : h - a.nq;
     float x[VEC], y[VEC];
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) x[e] = y[e] = 0.f;
-    if (on) {
-      const T* src = (isq ? (const T*)a.q + (size_t)r * a.ldq : (const T*)a.k + (size_t)r * a.ldk) + (size_t)hh * a.hd;
-      load_piece<T, VEC>(src + pa, x);
-      load_piece<T, VEC>(src + pb, y);
-    }
+    floats_of<T>(raw.a, x);
+    floats_of<T>(raw.b, y);
     if (a.gq || a.gk) {
       float s = 0.f;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) s = fmaf(x[e], x[e], fmaf(y[e], y[e], s));
-      for (int o = 1; o < lph; o *= 2) s += __shfl_xor(s, o);
+      for (int e = 0; e < VEC; ++e) s += (e >= dupx ? x[e] * x[e] : 0.f) + (e >= dupy ? y[e] * y[e] : 0.f);
+      s = sum_of_group(s, a.lph);
       const float* g = isq ? a.gq : a.gk;
       if (on && g) {
         const float f = 1.f / sqrtf(s / (float)a.hd + a.eps);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          x[e] = x[e] * f * g[pa + e];
-          y[e] = y[e] * f * g[pb + e];
-        }
+        scale_by<VEC>(x, f, g + pa, na);
+        scale_by<VEC>(y, f, g + pb, nb);
       }
     }
     if (!on) continue;
-    if (!a.style) {
-      if (u < turned) {
+    if (u < turned) {
+      if (!a.style) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
           const float l = x[e], m = y[e];
           x[e] = l * cs[e] - m * sn[e];
           y[e] = m * cs[e] + l * sn[e];
         }
-      }
-    } else {
+      } else {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        if (u * VEC + e >= a.dim / 2) continue;
-        // entries 2e, 2e + 1 of x and y after each other (one of each where VEC is 1)
-        float& l = VEC == 1 ? x[0] : 2 * e < VEC ? x[2 * e % VEC] : y[2 * e % VEC];
-        float& m = VEC == 1 ? y[0] : 2 * e < VEC ? x[(2 * e + 1) % VEC] : y[(2 * e + 1) % VEC];
-        const float l0 = l, m0 = m;
-        l = l0 * cs[e] - m0 * sn[e];
-        m = m0 * cs[e] + l0 * sn[e];
+        for (int e = 0; e < VEC; ++e) {
+          // entries 2e and 2e + 1 of x and y after each other
+          float& l = 2 * e < VEC ? x[2 * e % VEC] : y[2 * e % VEC];
+          float& m = 2 * e < VEC ? x[(2 * e + 1) % VEC] : y[(2 * e + 1) % VEC];
+          const float l0 = l, m0 = m;
+          l = l0 * cs[e] - m0 * sn[e];
+          m = m0 * cs[e] + l0 * sn[e];
+        }
       }
     }
     if (isq || !p.n_windows) {
       void* dst = isq ? a.qo : a.ko;
       const size_t at = (size_t)r * (isq ? a.ldqo : a.ldko) + (size_t)hh * a.hd;
-      store_piece<VEC>(dst, at + pa, a.bf16, x);
-      store_piece<VEC>(dst, at + pb, a.bf16, y);
-    } else if (page_row >= 0) {
-      const size_t base = (size_t)(page_row + (long long)hh * p.bpp) * 32 * a.hd + slot * 32;
-      store_piece<VEC>(p.k, base + (size_t)(pa >> 5) * 1024 + (pa & 31), p.kvb, x);
-      store_piece<VEC>(p.k, base + (size_t)(pb >> 5) * 1024 + (pb & 31), p.kvb, y);
+      store_piece<VEC>(dst, at + pa, a.bf16, na, x);
+      store_piece<VEC>(dst, at + pb, a.bf16, nb, y);
+    } else if (block >= 0) {
+      const size_t base = (size_t)(block + (long long)hh * p.bpp) * 32 * a.hd + slot * 32;
+      store_key<VEC>(p.k, base, pa, p.kvb, na, x);
+      store_key<VEC>(p.k, base, pb, p.kvb, nb, y);
     }
   }
 }
 
-template <typename T, int VEC>
+template <typename T>
 hipError_t launch(RotateArgs a, hipStream_t s) {
-  int lph = 1;
-  while (lph < a.hd / (2 * VEC)) lph *= 2;
-  const int heads = a.nq + a.nk, hpp = 64 / lph;
+  constexpr int VEC = Piece<T>::N;
+  const int units = (a.dim / 2 + VEC - 1) / VEC + (a.hd - a.dim + 2 * VEC - 1) / (2 * VEC);
+  a.lph = 1;
+  while (a.lph < units) a.lph *= 2;
+  const int heads = a.nq + a.nk, hpp = 64 / a.lph;
   a.passes = (heads + hpp - 1) / hpp;
-  // a row's waves share nothing: one pass each until the rows alone fill the card
-  const long long waves = (long long)a.rows * a.passes;
-  a.ppw = (int)std::min((long long)a.passes, std::max(1ll, waves / 8192));
-  a.wpr = (a.passes + a.ppw - 1) / a.ppw;
-  a.row_blocks = heads ? (int)(((long long)a.rows * a.wpr + kRotWaves - 1) / kRotWaves) : 0;
+  // waves of a row: one, or while the rows are few one for each group of heads
+  a.parts = (int)std::max(1ll, std::min((long long)a.passes, (long long)kRotFull / a.rows));
+  a.row_blocks = heads ? (int)(((long long)a.rows * a.parts + kRotWaves - 1) / kRotWaves) : 0;
   long long values = 0;
   if (a.pg.n_windows) {
     // blocks that the windows' rows touch, at most: 1 + (r - 1) / 32 rounded up of r rows
@@ -252,15 +356,12 @@ hipError_t launch(RotateArgs a, hipStream_t s) {
     values = (long long)a.pg.nkv * std::min((long long)a.rows, 2ll * n + (a.rows - n) / 32);
   }
   if (a.row_blocks + values < 1) return hipSuccess;
-  hipLaunchKernelGGL((k_rotate<T, VEC>), dim3((unsigned)(a.row_blocks + values)), dim3(kRotWaves * 64), 0, s, a);
+  hipLaunchKernelGGL((k_rotate<T>), dim3((unsigned)(a.row_blocks + values)), dim3(kRotWaves * 64), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_rotate(RotateArgs a, bool wide, hipStream_t s) {
-  if (a.bf16) return wide ? launch<uint16_t, 8>(a, s) : launch<uint16_t, 1>(a, s);
-  return wide ? launch<float, 4>(a, s) : launch<float, 1>(a, s);
-}
+hipError_t launch_rotate(RotateArgs a, hipStream_t s) { return a.bf16 ? launch<uint16_t>(a, s) : launch<float>(a, s); }
 
 }  // namespace dsi

@@ -2217,8 +2217,8 @@ static dsi_status rotate_args(RotateArgs& r, int rows, int nq, int nk, int hd, i
   r.gain = rope.gain;
   return DSI_OK;
 }
-// whether 16-byte pieces fit the rows at p, ld entries apart
-static bool wide_rows(const void* p, size_t ld, size_t esz) { return aligned(p, 16) && ld * esz % 16 == 0; }
+// whether the rows at p, ld entries apart, are 16-byte aligned
+static bool rows_aligned(const void* p, size_t ld, size_t esz) { return aligned(p, 16) && ld * esz % 16 == 0; }
 
 dsi_status dsi_rotate(void* stream, const dsi_rotate_args* a) {
   if (!a) return fail(DSI_EINVAL, "null argument");
@@ -2228,14 +2228,12 @@ dsi_status dsi_rotate(void* stream, const dsi_rotate_args* a) {
   if (!a->rows || a->n_heads + a->n_kv_heads == 0) return DSI_OK;
   if (a->rope.dim && !a->d_pos) return fail(DSI_EINVAL, "null positions");
   const size_t esz = r.bf16 ? 2 : 4;
-  bool wide = r.style || r.dim % (32 / (int)esz) == 0;
   auto part = [&](const char* what, int heads, const void* in, int64_t ld, void* out, int64_t ld_out) -> dsi_status {
     if (!heads) return DSI_OK;
     const long long n = (long long)heads * a->head_dim;
     DSI_TRY(rows_ok(what, in, ld, n, esz));
     DSI_TRY(rows_ok(what, out, ld_out, n, esz));
     DSI_TRY(apart_ok(what, in, ld, out, ld_out, a->rows, n, esz));
-    wide = wide && wide_rows(in, ld, esz) && wide_rows(out, ld_out, esz);
     return DSI_OK;
   };
   DSI_TRY(part("queries", a->n_heads, a->d_q, a->ld_q, a->d_q_out, a->ld_q_out));
@@ -2248,7 +2246,7 @@ dsi_status dsi_rotate(void* stream, const dsi_rotate_args* a) {
   r.ldk = (size_t)a->ld_k;
   r.ldqo = (size_t)a->ld_q_out;
   r.ldko = (size_t)a->ld_k_out;
-  HIP_TRY(launch_rotate(r, wide, (hipStream_t)stream));
+  HIP_TRY(launch_rotate(r, (hipStream_t)stream));
   return DSI_OK;
 }
 
@@ -2296,16 +2294,13 @@ dsi_status dsi_page_append(void* stream, const dsi_pages* pages, const dsi_page_
   DSI_TRY(page_pointers_ok(pages));
   const size_t esz = r.bf16 ? 2 : 4;
   const long long nq = (long long)a->n_heads * r.hd, nk = (long long)r.nk * r.hd;
-  bool wide = r.style || r.dim % (32 / (int)esz) == 0;
   if (a->n_heads) {
     DSI_TRY(rows_ok("queries", a->d_q, a->ld_q, nq, esz));
     DSI_TRY(rows_ok("output", a->d_q_out, a->ld_q_out, nq, esz));
     DSI_TRY(apart_ok("queries", a->d_q, a->ld_q, a->d_q_out, a->ld_q_out, a->rows, nq, esz));
-    wide = wide && wide_rows(a->d_q, a->ld_q, esz) && wide_rows(a->d_q_out, a->ld_q_out, esz);
   }
   DSI_TRY(rows_ok("keys", a->d_k, a->ld_k, nk, esz));
   DSI_TRY(rows_ok("values", a->d_v, a->ld_v, nk, esz));
-  wide = wide && wide_rows(a->d_k, a->ld_k, esz) && wide_rows(a->d_v, a->ld_v, esz);
   r.nv = r.nk;
   r.q = a->d_q;
   r.k = a->d_k;
@@ -2315,7 +2310,7 @@ dsi_status dsi_page_append(void* stream, const dsi_pages* pages, const dsi_page_
   r.ldk = (size_t)a->ld_k;
   r.ldv = (size_t)a->ld_v;
   r.ldqo = (size_t)a->ld_q_out;
-  HIP_TRY(launch_rotate(r, wide, (hipStream_t)stream));
+  HIP_TRY(launch_rotate(r, (hipStream_t)stream));
   return DSI_OK;
 }
 
@@ -2350,7 +2345,7 @@ dsi_status dsi_page_attend(void* stream, const dsi_pages* pages, const dsi_page_
   const long long n = (long long)a->n_heads * pages->head_dim;
   DSI_TRY(rows_ok("queries", a->d_q, a->ld_q, n, esz));
   DSI_TRY(rows_ok("output", a->d_out, a->ld_out, n, esz));
-  if (!wide_rows(a->d_q, (size_t)a->ld_q, esz) || !wide_rows(a->d_out, (size_t)a->ld_out, esz))
+  if (!rows_aligned(a->d_q, (size_t)a->ld_q, esz) || !rows_aligned(a->d_out, (size_t)a->ld_out, esz))
     return fail(DSI_EINVAL, "rows of queries and output must be 16-byte aligned");
   if (a->d_q == a->d_out) return fail(DSI_EINVAL, "d_out overlaps d_q");
   DSI_TRY(apart_ok("queries", a->d_q, a->ld_q, a->d_out, a->ld_out, a->rows, n, esz));

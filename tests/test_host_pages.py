@@ -75,13 +75,16 @@ def test_rotate_refusals(stub):
         dsi.dsi_rotate(0, rows, hq, hkv, hd, 1 << 20, 2 << 20, P, 3 << 20, 4 << 20, k.pop("rope", rope), dtype, **k)
         (name, args, g), = launches()
         return g[0]
-    assert grid(place := 1, 32, 8) > 0
+    assert grid(1, 32, 8) > 0
     dsi.dsi_rotate(0, 5, 4, 2, 64, 1 << 20, 2 << 20, P, 1 << 20, 2 << 20, rope)          # in place
     dsi.dsi_rotate(0, 5, 4, 2, 64, 1 << 20, 2 << 20, None, 3 << 20, 4 << 20, dsi.make_rope(0, None))   # norms alone
-    # every wave of a row is there: heads / heads of a wave, four waves a workgroup
-    assert grid(1, 32, 8, 64) == -(-(-(-40 // 8)) // 4) and grid(1, 40, 40, 128) == -(-(-(-80 // 4)) // 4)
-    assert grid(1, 32, 8, 64, 1) == -(-(-(-40 // 16)) // 4)
-    assert grid(1, 32, 8, 64, rope=dsi.make_rope(30, P)) == -(-(-(-40 // 2)) // 4)       # pieces of one entry
+    # groups of heads that a wave takes at a time: 64 lanes of 16 bytes a half
+    groups = lambda heads, per: -(-heads // per)
+    assert grid(1, 32, 8, 64) == -(-groups(40, 8) // 4) and grid(1, 40, 40, 128) == -(-groups(80, 4) // 4)
+    assert grid(1, 32, 8, 64, 1) == -(-groups(40, 16) // 4)
+    # 15 pairs in four lanes, 34 entries that are not turned in five: 16 lanes a head
+    assert grid(1, 32, 8, 64, rope=dsi.make_rope(30, P)) == -(-groups(40, 4) // 4)
+    assert grid(5000, 40, 40, 128) == 5000
     assert not hip.stub_mallocs()
     ''')
 
