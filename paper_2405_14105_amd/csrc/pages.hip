@@ -588,10 +588,11 @@ struct ManyShared {
   static constexpr int FB = DS + 2 * DT, FR = KS * FB;     // fragments of a block, of a stage
   u32x4 kv[2][FR][FP][64];
 };
-// 16 bytes a lane from memory into LDS, lane by lane from `to` on, past the
-// registers; in order with the wave's loads, and complete once vmcnt says so
-__device__ __forceinline__ void load_lds(const void* from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+// 16 bytes a lane from memory (`off` bytes behind `from`, by the lane) into LDS, lane
+// by lane from `to` on, past the registers; in order with the wave's loads, and
+// complete once vmcnt says so
+__device__ __forceinline__ void load_lds(const void* from, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(from), "s"(to) : "memory");
 }
 template <bool KVB, int HD, bool QB>
 __device__ __forceinline__ void many_item(const PageAttnArgs& a, const PageClass& cl, int block, ManyShared<KVB, HD>& sh) {
@@ -622,13 +623,21 @@ __device__ __forceinline__ void many_item(const PageAttnArgs& a, const PageClass
     const int kb = kb0 + i0 + lane;
     mine = kb < kb1 ? (int)block_of(a.pg, it.b, kvh, kb) : -1;
   };
-  look(0);
   int row, g, pos;
   query_at(a, it.w, x0 + q32, row, g, pos);
   const int from = a.reach ? pos - a.reach + 1 : 0;
   u32x4 q[DS][QT];
 #pragma unroll
   for (int ds = 0; ds < DS; ++ds) load_query<KVB, QB>(a, (size_t)row * a.ldq + (size_t)(kvh * a.G + g) * HD + ds * 16 + hh * 8, q[ds]);
+
+  // all that the wave loaded into registers is there: what it waits for in the loop
+  // must not be the next stage
+  look(0);
+#pragma unroll
+  for (int ds = 0; ds < DS; ++ds)
+#pragma unroll
+    for (int i = 0; i < QT; ++i) asm volatile("" : "+v"(q[ds][i]));
+  asm volatile("" : "+v"(mine));
 
   const uint32_t lds = (uint32_t)(size_t)(__attribute__((address_space(3))) void*)&sh.kv[0][0][0][0];
   // of a block without a page, or past the last, block 0 of the pool is read, and masked
@@ -637,10 +646,11 @@ __device__ __forceinline__ void many_item(const PageAttnArgs& a, const PageClass
     for (int j = 0; j < MINE; ++j) {
       const int f = w + NW * j, n = KS == 1 ? 0 : f / FB, r = f - n * FB;
       if (FR % NW && f >= FR) continue;
-      const size_t at = (size_t)max(b[n], 0) * (32 * HD) + (r < DS ? key_offset(lane, r) : value_offset(lane, (r - DS) >> 1, (r - DS) & 1));
+      const size_t at = (size_t)max(b[n], 0) * (32 * HD) + (r < DS ? key_offset(0, r) : value_offset(0, (r - DS) >> 1, (r - DS) & 1));
       const char* src = (const char*)(r < DS ? a.pg.k : a.pg.v) + at * (KVB ? 2 : 4);
+      const uint32_t off = (uint32_t)(r < DS ? key_offset(lane, 0) : value_offset(lane, 0, 0)) * (KVB ? 2 : 4);
 #pragma unroll
-      for (int i = 0; i < FP; ++i) load_lds(src + 16 * i, lds + (uint32_t)(((buf * FR + f) * FP + i) * 1024));
+      for (int i = 0; i < FP; ++i) load_lds(src + 16 * i, off, lds + (uint32_t)(((buf * FR + f) * FP + i) * 1024));
     }
   };
   auto frag = [&](int buf, int f) {
@@ -687,12 +697,14 @@ __device__ __forceinline__ void many_item(const PageAttnArgs& a, const PageClass
     }
     if (live && p0 <= my.last && p0 + 32 * KS - 1 >= my.lo) {
       f32x16 s[KS];
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int n = 0; n < KS; ++n) {
-        s[n] = zero16();
+      for (int n = 0; n < KS; ++n) s[n] = zero16();
 #pragma unroll
-        for (int ds = 0; ds < DS; ++ds) scores<KVB>(s[n], frag(buf, n * FB + ds), q[ds]);
-      }
+      for (int ds = 0; ds < DS; ++ds)
+#pragma unroll
+        for (int n = 0; n < KS; ++n) scores<KVB>(s[n], frag(buf, n * FB + ds), q[ds]);
+      __builtin_amdgcn_s_setprio(0);
       // not every query sees every key
       bool some = p0 + 32 * KS - 1 > my.first || (a.reach && p0 <= my.last - a.reach);
 #pragma unroll
@@ -711,8 +723,10 @@ __device__ __forceinline__ void many_item(const PageAttnArgs& a, const PageClass
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[t] *= alpha;
       }
+      __builtin_amdgcn_s_setprio(1);
       if (__builtin_expect(some, 0)) values(std::true_type{}, s, vis, buf);
       else values(std::false_type{}, s, vis, buf);
+      __builtin_amdgcn_s_setprio(0);
     }
 #pragma unroll
     for (int n = 0; n < KS; ++n) b[n] = next[n];
@@ -759,8 +773,11 @@ __global__ __launch_bounds__(256, KVB || HD < 128 ? 2 : 1) void k_page_few(PageA
   __shared__ FewShared<KVB, HD, QB> sh;
   few_items<KVB, HD, QB>(a, cl, blockIdx.x, gridDim.x, sh);
 }
+// Two workgroups fit a CU but where fp32 queries or keys of wide heads take more than
+// 256 registers.
+constexpr bool many_two(bool kvb, int hd, bool qb) { return hd <= 64 || (kvb && qb); }
 template <bool KVB, int HD, bool QB>
-__global__ __launch_bounds__(256, QB && KVB ? 2 : 1) void k_page_many(PageAttnArgs a, PageClass cl) {
+__global__ __launch_bounds__(256, many_two(KVB, HD, QB) ? 2 : 1) void k_page_many(PageAttnArgs a, PageClass cl) {
   __shared__ ManyShared<KVB, HD> sh;
   many_item<KVB, HD, QB>(a, cl, blockIdx.x, sh);
 }
@@ -898,7 +915,7 @@ Classes classes_of(const PageArgs& pg, int rows, int nq, bool bf16) {
   c.many.qlo = c.use_few ? 65 : 1;
   c.many.qhi = INT_MAX;
   c.many.qw = 4;
-  c.many.once = c.many.most = 4 * (bf16 && pg.kvb ? kSlots : kSlots / 2);
+  c.many.once = c.many.most = 4 * (many_two(pg.kvb, pg.hd, bf16) ? kSlots : kSlots / 2);
   c.many.enough = INT_MAX;
   for (PageClass* cl : {&c.few, &c.many}) {
     cl->inv_once = 1.0 / cl->once;   // powers of two: exact

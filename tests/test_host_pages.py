@@ -72,7 +72,7 @@ def test_rotate_refusals(stub):
     rope = dsi.make_rope(64, P)
     def grid(rows=5, hq=4, hkv=2, hd=64, dtype=0, **k):
         hip.stub_clear()
-        dsi.dsi_rotate(0, rows, hq, hkv, hd, 1 << 20, 2 << 20, P, 3 << 20, 4 << 20, k.pop("rope", rope), dtype, **k)
+        dsi.dsi_rotate(0, rows, hq, hkv, hd, 1 << 30, 2 << 30, P, 3 << 30, 4 << 30, k.pop("rope", rope), dtype, **k)
         (name, args, g), = launches()
         return g[0]
     assert grid(1, 32, 8) > 0
@@ -84,7 +84,7 @@ def test_rotate_refusals(stub):
     assert grid(1, 32, 8, 64, 1) == -(-groups(40, 16) // 4)
     # 15 pairs in four lanes, 34 entries that are not turned in five: 16 lanes a head
     assert grid(1, 32, 8, 64, rope=dsi.make_rope(30, P)) == -(-groups(40, 4) // 4)
-    assert grid(5000, 40, 40, 128) == 5000
+    assert grid(5000, 40, 40, 128) == 1250
     assert not hip.stub_mallocs()
     ''')
 
