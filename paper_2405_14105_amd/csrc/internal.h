@@ -535,8 +535,9 @@ struct PageClass {
   // long as an item then has no more than `enough` units of keys, up to `most`
   int once, most, enough;
   double inv_once, inv_most;
-  float* part;          // [slots][32][head_dim]
-  float2* ml;           // [slots][32]: maximum (base 2) and sum
+  int slots;            // of a KV head, for the parts of tiles that are cut
+  float* part;          // [slots][nkv][32][head_dim]
+  float2* ml;           // [slots][nkv][32]: maximum (base 2) and sum
 };
 size_t page_attend_workspace_bytes(const PageArgs& pg, int rows, int nq);
 hipError_t launch_page_attend(const PageAttnArgs& a, void* ws, hipStream_t s);

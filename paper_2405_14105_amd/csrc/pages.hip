@@ -62,7 +62,7 @@ __device__ __forceinline__ Win window_at(const PageAttnArgs& a, const PageClass&
   const int T = 32 * w.qw;
   w.tiles = (unsigned)(queries + T - 1) / (unsigned)T;
   int span = w.bad ? 1 : w.len + w.R;
-  if (a.reach) span = min(span, a.reach + (int)((unsigned)(T + a.G - 2) / (unsigned)a.G)) + 31;   // a tile's rows, from a block's first position on
+  if (a.reach) span = min(span, a.reach + (int)((unsigned)(T + a.G - 2) / (unsigned)a.G) + 31);   // a tile's rows, from a block's first position on
   w.units = (span + kUnit - 1) / kUnit;
   return w;
 }
@@ -105,7 +105,7 @@ __device__ __forceinline__ Plan plan_of(const PageAttnArgs& a, const PageClass& 
   const double once = ceil(work * cl.inv_once), fine = ceil(work * cl.inv_most);
   p.per = (int)fmin(fmax(fmax(fine, fmin(once, (double)cl.enough)), 1.0), 1e9);
   // chunks are whole: a few units more where they are a few items too many for one turn
-  if (whole && once <= cl.enough) {
+  if (whole && once <= cl.enough && (long long)wave_total(p.w.tiles * p.w.qw) * a.pg.nkv <= cl.once) {
     for (int i = 0; i < 6; ++i) {
       const int items = wave_total(p.w.tiles * p.w.qw * chunks_of(p.w.units, p.per));
       if ((long long)items * a.pg.nkv <= cl.once) break;
@@ -155,6 +155,8 @@ __device__ __forceinline__ bool find(const PageAttnArgs& a, const PageClass& cl,
         it.sub = 0;
       }
       it.slot = slots + at(p.sincl - p.split) + it.tile * it.chunks * it.w.qw;
+      // rows of windows that overlap may need more than there are: no output (NaN)
+      if (it.chunks > 1 && it.slot + it.chunks * it.w.qw > cl.slots) it.w.bad = 1;
       return true;
     }
     t -= __builtin_amdgcn_readlane(p.incl, 63);
@@ -796,7 +798,7 @@ __global__ __launch_bounds__(256) void k_page_join(PageAttnArgs a, PageClass few
   const int gr = threadIdx.x / PER, d = threadIdx.x % PER;
   auto join = [&](const PageClass& cl, const Item& it, int kvh, int part) {
     const int qw = it.w.qw, T = 32 * qw, x0 = it.tile * T + it.sub * 32 + part * kJoinQ;
-    const int live = min(kJoinQ, it.w.R * a.G - x0);
+    const int live = it.w.bad ? 0 : min(kJoinQ, it.w.R * a.G - x0);
     if (live < 1) return;
     const Span sp = span_of(a, it.w, it.tile * T, T);
     const int units = (sp.hi - sp.lo + kUnit - 1) / kUnit;
@@ -890,8 +892,14 @@ long long most_tiles(const PageArgs& pg, int rows, int nq, int qw) {
   return n + (queries - n) / (32 * qw);
 }
 // Slots (32 queries of an item of a tile that is cut): tiles * qw * chunks of them are
-// less than twice tiles * qw * units / per, which is at most `most`
-long long slots(const PageClass& c) { return 2ll * c.most; }
+// less than twice tiles * qw * units / per, which is at most `most`; and no tile has
+// more chunks than the windows' pages have units
+long long slots(const PageClass& c, const PageArgs& pg, int rows, int nq) {
+  const int qw = c.qw ? c.qw : 1, windows = std::min(pg.n_windows, rows);
+  const long long units = ((long long)pg.max_pages * pg.bpp * 32 + kUnit - 1) / kUnit;
+  const long long tiles = most_tiles(pg, rows, nq, qw) * qw + windows;   // of 32 queries, the last of a window's tile empty
+  return std::min(2ll * c.most, tiles * pg.nkv * units);
+}
 
 constexpr int kSlots = 512;   // workgroups that the card holds at once, two a CU
 constexpr int kJoinGrid = 1024;
@@ -930,9 +938,11 @@ hipError_t launch_all(PageAttnArgs a, void* ws, hipStream_t s) {
   char* at = (char*)ws;
   for (PageClass* cl : {&c.few, &c.many}) {
     if (cl == &c.few ? !c.use_few : !c.use_many) continue;
+    const long long n = slots(*cl, a.pg, a.rows, a.nq);
+    cl->slots = (int)(n / a.pg.nkv);
     cl->ml = (float2*)at;
-    cl->part = (float*)(cl->ml + slots(*cl) * 32);
-    at = (char*)(cl->part + slots(*cl) * 32 * HD);
+    cl->part = (float*)(cl->ml + n * 32);
+    at = (char*)(cl->part + n * 32 * HD);
   }
   const int nkv = a.pg.nkv, windows = std::min(a.pg.n_windows, a.rows);
   long long nfew = 0, nmany = 0, jfew = 0, jmany = 0;
@@ -976,7 +986,7 @@ size_t page_attend_workspace_bytes(const PageArgs& pg, int rows, int nq) {
   size_t most = 0;
   for (bool bf16 : {false, true}) {   // whatever the call's type
     const Classes c = classes_of(pg, rows, nq, bf16);
-    most = std::max(most, (size_t)((c.use_few ? slots(c.few) : 0) + (c.use_many ? slots(c.many) : 0)));
+    most = std::max(most, (size_t)((c.use_few ? slots(c.few, pg, rows, nq) : 0) + (c.use_many ? slots(c.many, pg, rows, nq) : 0)));
   }
   return most * 32 * (pg.hd * sizeof(float) + sizeof(float2));
 }

@@ -2173,14 +2173,19 @@ static dsi_status rows_ok(const char* what, const void* p, int64_t ld, long long
     return fail(DSI_EINVAL, "%s: rows of %lld entries lie %lld apart", what, entries, (long long)ld);
   return DSI_OK;
 }
-// in place, or apart
+// in place, or apart (columns of one buffer among others)
 static dsi_status apart_ok(const char* what, const void* in, int64_t ld_in, const void* out, int64_t ld_out, int rows,
                            long long entries, size_t esz) {
   if (in == out && ld_in == ld_out) return DSI_OK;
   const uintptr_t i0 = (uintptr_t)in, o0 = (uintptr_t)out;
-  const uintptr_t i1 = i0 + ((size_t)(rows - 1) * ld_in + entries) * esz, o1 = o0 + ((size_t)(rows - 1) * ld_out + entries) * esz;
-  if (i0 < o1 && o0 < i1) return fail(DSI_EINVAL, "%s overlaps its output without being in place", what);
-  return DSI_OK;
+  const size_t n = (size_t)entries * esz, step = (size_t)ld_in * esz;
+  const uintptr_t i1 = i0 + (size_t)(rows - 1) * step + n, o1 = o0 + (size_t)(rows - 1) * ld_out * esz + n;
+  if (i0 >= o1 || o0 >= i1) return DSI_OK;
+  if (ld_in == ld_out) {   // how far an output's row lies behind an input's
+    const size_t d = o0 >= i0 ? (o0 - i0) % step : (step - (i0 - o0) % step) % step;
+    if (d >= n && d + n <= step) return DSI_OK;
+  }
+  return fail(DSI_EINVAL, "%s overlaps its output without being in place", what);
 }
 
 static dsi_status rope_ok(const dsi_rope& r, int hd) {

@@ -86,7 +86,7 @@ def test_rows(rows):
     check(Step(rows, [50 * (b + 1) for b in range(len(rows))], 2, 32, BF16, 64, seed=len(rows), before=3, behind=4), 6, F32)
 
 
-@pytest.mark.parametrize("reach", [1, 2, 31, 32, 33, 100, 5000])
+@pytest.mark.parametrize("reach", [1, 2, 31, 32, 33, 100, 900, 5000])
 @pytest.mark.parametrize("kv", [F32, BF16])
 def test_reach(reach, kv):
     """Pages before every row's reach are not in the table, positions before it are NaN."""
@@ -177,6 +177,15 @@ def test_rows_of_windows_that_are_out_of_order_stay_in_bounds():
     attend(step, torch.randn((step.n, 256), device="cuda"), 4)
 
 
+def test_rows_of_windows_that_overlap_stay_in_bounds():
+    """Eight windows that all claim the step's rows: more parts than the workspace of these sizes has."""
+    for rows, hq in ((4, 4), (64, 16)):
+        step = Step([rows] + [0] * 7, [480 - rows] * 8, 2, 64, BF16, 32).to("cuda")
+        step.table[:] = step.table[0]
+        step.row0 = torch.tensor([0, rows, 0, rows, 0, rows, 0, rows, 0], dtype=torch.int32, device="cuda")
+        attend(step, torch.randn((step.n, hq * 64), device="cuda"), hq)
+
+
 @pytest.mark.parametrize("rows", [[1, 4, 40], [1, 4, 170]])
 def test_one_call_gives_the_same_bits(rows):
     step = Step(rows, [3000, 17, 500], 2, 128, BF16, 64).to("cuda")
@@ -215,3 +224,63 @@ def test_captured_and_replayed_with_other_lengths():
         torch.cuda.synchronize()
         # bits: rows that see positions the pool does not hold are NaN both times
         assert torch.equal(out.view(torch.int32), attend(step, q, hq, pages=pages).view(torch.int32))
+
+
+def test_pools_beyond_32_bit_offsets():
+    """Pages behind 2^31 entries of a pool: read by few and many rows, and appended to."""
+    hq, hkv, hd, page = 8, 8, 128, 256
+    step = Step([2, 40], [600, 10], hkv, hd, BF16, page)
+    q = torch.randn((step.n, hq, hd), generator=torch.Generator().manual_seed(1))
+    ref, mass, big = attend64(step, q, hq)
+    n = step.k.shape[0]
+    pages = 2 ** 31 // step.k[0].numel() + 2 * n
+    k, v = (torch.empty((pages, *x.shape[1:]), dtype=BF16, device="cuda") for x in (step.k, step.v))
+    k[-n:], v[-n:] = step.k.cuda(), step.v.cuda()
+    step.k, step.v = k, v
+    step.table = torch.where(step.table >= 0, step.table + pages - n, step.table)
+    step.to("cuda")
+    got = attend(step, q.view(step.n, -1).cuda(), hq).cpu().view(step.n, hq, hd)
+    assert ((got.double() - ref).abs() <= tolerance(step, ref, mass, big, F32)).all()
+    new = torch.randn((step.n, hkv * hd), device="cuda")
+    first = k[:4].clone(), v[:4].clone()
+    dsi.dsi_page_append(torch.cuda.current_stream().cuda_stream, step.pages(), step.n, 0, None, new, new, None, dsi.make_rope(0, None))
+    torch.cuda.synchronize()
+    for b, r0 in ((0, 0), (1, 2)):
+        at = torch.arange(step.past[b], step.past[b] + step.rows[b], device="cuda")
+        where, place = step.table[b].long()[at // page], at % page
+        rows = new[r0:r0 + step.rows[b]].view(-1, hkv, hd).to(BF16)
+        assert torch.equal(k[where, :, place // 32, :, place % 32].reshape(-1, hkv, hd), rows)
+        assert torch.equal(v[where, :, place // 32, :, place % 32], rows)
+    assert torch.equal(k[:4].view(torch.int16), first[0].view(torch.int16)) and torch.equal(v[:4].view(torch.int16), first[1].view(torch.int16))
+
+
+def test_rows_among_others_and_another_stream():
+    """Queries and outputs as columns of one buffer, on a stream of the caller's."""
+    hq, hd = 4, 64
+    step = Step([3, 90], [40, 7], 2, hd, BF16, 32)
+    buf = torch.randn((step.n, 2 * hq * hd + 64), generator=torch.Generator().manual_seed(2))
+    ref, mass, big = attend64(step, buf[:, :hq * hd].view(step.n, hq, hd), hq)
+    step.to("cuda")
+    side, d = torch.cuda.Stream(), buf.cuda()
+    torch.cuda.synchronize()
+    attend(step, d[:, :hq * hd], hq, stream=side, out=d[:, hq * hd:2 * hq * hd])
+    got = d.cpu()
+    assert torch.equal(got[:, :hq * hd], buf[:, :hq * hd]) and torch.equal(got[:, 2 * hq * hd:], buf[:, 2 * hq * hd:])
+    assert ((got[:, hq * hd:2 * hq * hd].view(step.n, hq, hd).double() - ref).abs() <= tolerance(step, ref, mass, big, F32)).all()
+
+
+def test_two_calls_at_once():
+    """Calls on two streams with workspaces of their own."""
+    hq = 8
+    steps = [Step([1, 4, 60], [5000 + 7 * i, 17, 900], 2, 64, BF16, 64, seed=i).to("cuda") for i in range(2)]
+    qs = [torch.randn((s.n, hq * 64), device="cuda") for s in steps]
+    want = [attend(s, q, hq) for s, q in zip(steps, qs)]
+    outs, streams = [torch.zeros_like(q) for q in qs], [torch.cuda.Stream() for _ in steps]
+    sizes = [dsi.dsi_page_attend_workspace(s.pages(), s.n, hq) for s in steps]
+    ws = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            dsi.dsi_page_attend(streams[i].cuda_stream, steps[i].pages(), steps[i].n, hq, qs[i], outs[i], ws[i], sizes[i])
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])

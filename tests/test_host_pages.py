@@ -129,8 +129,16 @@ def test_attend_refusals_and_workspace():
     assert lib.dsi_page_attend(None, None, None) == dsi.DSI_EINVAL
     wide = dsi.make_pages(**{**PAGES, "n_kv_heads": 1})
     refused(dsi.dsi_page_attend_workspace, dict(pages=wide, rows=1 << 22, n_heads=64), dict(n_heads=65))
-    # a workspace holds the parts of tiles that are cut, however many rows there are
-    assert dsi.dsi_page_attend_workspace(pages, 1 << 22, 4) <= 600 << 20
+    # a workspace holds the parts of tiles that are cut, however many rows there are, and of no more chunks than
+    # the pages have units of 128 keys
+    slot = 32 * (64 * 4 + 8)
+    assert dsi.dsi_page_attend_workspace(pages, 1 << 22, 4) == 2 * 2 * 2048 * slot
+    assert dsi.dsi_page_attend_workspace(pages, 1, 4) == (1 + 1) * 2 * 4 * slot
+    long = dsi.make_pages(**{**PAGES, "max_pages": 1 << 20})
+    assert dsi.dsi_page_attend_workspace(long, 1, 4) == 2 * 2048 * slot
+    # rows of the output may lie among those of the queries
+    dsi_rows = dict(ok, d_q=1 << 20, d_out=(1 << 20) + 256 * 4, ld_q=600, ld_out=600)
+    refused(dsi.dsi_page_attend, dsi_rows, dict(d_out=(1 << 20) + 255 * 4), dict(d_out=(1 << 20) + 348 * 4), dict(ld_out=604))
 
 
 def test_adjust_refusals(stub):
