@@ -784,6 +784,21 @@ __global__ __launch_bounds__(256, many_two(KVB, HD, QB) ? 2 : 1) void k_page_man
   many_item<KVB, HD, QB>(a, cl, blockIdx.x, sh);
 }
 
+// Both in one launch where two workgroups of either fit a CU: those for few rows come
+// first, one for each CU, and items of many rows beside them.  (1B, 500 rows beside
+// 15 single ones: 39 us one after the other, 33 together; 8B, 300 beside 8 x 6: 40 and
+// 28; 13B, 512 beside 7: 134 and 131, both bound by the memory by then.)
+template <bool KVB, int HD, bool QB>
+__global__ __launch_bounds__(256, 2) void k_page_both(PageAttnArgs a, PageClass few, PageClass many, int nfew) {
+  __shared__ union Both {
+    ManyShared<KVB, HD> m;
+    FewShared<KVB, HD, QB> f;
+    __device__ Both() {}
+  } sh;
+  if ((int)blockIdx.x < nfew) few_items<KVB, HD, QB>(a, few, blockIdx.x, nfew, sh.f);
+  else many_item<KVB, HD, QB>(a, many, (int)blockIdx.x - nfew, sh.m);
+}
+
 // ------------------------------------------------------------------ the join
 
 // Eight queries of a tile of several chunks: HD / 4 threads hold a query's outputs,
@@ -958,10 +973,20 @@ hipError_t launch_all(PageAttnArgs a, void* ws, hipStream_t s) {
     jmany = std::min(tiles * 4, (long long)c.many.most / nkv + 1);
   }
   if (nmany > INT_MAX) return hipErrorInvalidValue;
-  if (nmany) hipLaunchKernelGGL((k_page_many<KVB, HD, QB>), dim3((unsigned)nmany), dim3(256), 0, s, a, c.many);
+  bool both = false;
+  if constexpr (many_two(KVB, HD, QB)) {
+    both = nfew && nmany;
+    if (both) {
+      nfew = std::min(nfew, (long long)kSlots / 2);
+      c.few.once = kSlots / 2;
+      c.few.inv_once = 1.0 / c.few.once;
+      hipLaunchKernelGGL((k_page_both<KVB, HD, QB>), dim3((unsigned)(nfew + nmany)), dim3(256), 0, s, a, c.few, c.many, (int)nfew);
+    }
+  }
+  if (nmany && !both) hipLaunchKernelGGL((k_page_many<KVB, HD, QB>), dim3((unsigned)nmany), dim3(256), 0, s, a, c.many);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (nfew) hipLaunchKernelGGL((k_page_few<KVB, HD, QB>), dim3((unsigned)nfew), dim3(256), 0, s, a, c.few);
+  if (nfew && !both) hipLaunchKernelGGL((k_page_few<KVB, HD, QB>), dim3((unsigned)nfew), dim3(256), 0, s, a, c.few);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const long long joins = (jfew + jmany) * nkv * (32 / kJoinQ);
