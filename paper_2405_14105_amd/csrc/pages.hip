@@ -6,12 +6,14 @@
 // * G + head of the group), so that tiles of queries are full whatever the
 // group; a tile's keys are cut into chunks, an item is one chunk of one tile and
 // KV head.  Lengths are the device's: every workgroup works out the cut itself
-// from the windows' lengths and rows, so that items are about equally long and
-// about `target` in number whatever the windows are.
+// from the windows' lengths and rows (about 2 us), so that items are about equally
+// long and as many as the card takes whatever the windows are.
 // S^T = K Q^T and O^T = V^T P^T in 32 x 32 x 16 MFMAs: the rows of the K operand
 // are taken in an order in which a lane's scores are already its fragments of
 // P^T, and a block's layout is such that every operand is 16 contiguous bytes.
 // Parts of a tile are joined by a second launch.
+// Windows of up to 64 queries of a KV head (few rows) are bound by reading the pages,
+// others by the matrix cores: two kernels, or one launch of both.
 #include <algorithm>
 #include <type_traits>
 
@@ -418,10 +420,14 @@ __device__ __forceinline__ void store_nan(const PageAttnArgs& a, const Item& it,
 // chunk's blocks of 32 keys in turn (four waves a block apart, or two pairs), each
 // with a maximum, a sum and outputs of its own; they meet in LDS at the end.  A
 // block's keys and values go from memory to registers, the next block's while
-// this one's are worked on; queries lie in LDS in fragment order.  Bound by
-// reading the pages.
-// A query over a bf16 cache is one bf16 part or three, a probability two or
-// three; fp32 caches take fp32 MFMAs.
+// this one's are worked on; queries lie in LDS in fragment order.
+// Bound by reading the pages: 8B, 32 single rows over 100 to 31131 positions (2.05 GB)
+// 352 us, 5.8 TB/s.  Few and short windows are bound by a chain of loads (rows and
+// lengths, table, keys) and the meeting of the waves: 4 rows of 1B over up to 512
+// positions 8.3 us, 7 x 6 fp32 rows of 8B over 2048 (61 MB) 18.5.  64 queries in one
+// wave took 65 us there, with the spills of its 128 outputs a lane.
+// A query over a bf16 cache is one bf16 part, or three for fp32 queries (exact); a
+// probability two, 2^-16 of it left, or three; fp32 caches take fp32 MFMAs.
 template <bool KVB, int HD, bool QB>
 struct FewShared {
   static constexpr int QT = KVB ? (QB ? 1 : 3) : 2, DS = HD / 16, OS = HD + 4;
@@ -582,8 +588,15 @@ __device__ __forceinline__ void few_item(const PageAttnArgs& a, const PageClass&
 // them the same stages of KS blocks of 32 keys, which go through LDS in fragment
 // order, the next one's on their way while one is worked on.  Queries stay in
 // registers.  Bound by the matrix cores, the fragment reads from LDS and the
-// exponentials.
-// The probabilities of bf16 queries are rounded to bf16 (2^-8, as the outputs are).
+// exponentials: 8B, 2048 rows after 30000 positions 1.10 ms, 0.95 PFLOP/s, where a
+// large library product reaches 1.14.  (Fragments from memory to registers, each wave
+// its own: 1.88 ms.  Eight waves and stages through registers: 1.28.  Four waves that
+// way: 2.87, out of registers.)  A wave's loads of its queries have to be waited for
+// before the loop: the compiler's wait for them in it would be one for the stage just
+// asked for.
+// The probabilities of bf16 queries are rounded to bf16 (2^-8, as the outputs are):
+// a second part would be half as many matrix instructions again, and what it saves
+// (outputs off by 2.0e-3 of their norm against 1.7e-3) is less than their own rounding.
 template <bool KVB, int HD>
 struct ManyShared {
   static constexpr int KS = KVB ? 2 : 1, FP = KVB ? 1 : 2, DS = HD / 16, DT = HD / 32;
@@ -917,25 +930,33 @@ long long slots(const PageClass& c, const PageArgs& pg, int rows, int nq) {
 }
 
 constexpr int kSlots = 512;   // workgroups that the card holds at once, two a CU
-constexpr int kJoinGrid = 1024;
+constexpr int kJoinGrid = 1024;   // of the join, which takes parts in turn (512: 32 decoding windows 8.8 us, 1024 8.0)
 
 struct Classes {
   PageClass few, many;
   bool use_few, use_many;
 };
-// Windows of up to 64 queries of a KV head are few rows.  A call that has no more
-// than kAllFew in all, or a single window, takes one kind for all its windows.
+// Windows of up to kFewQueries queries of a KV head are few rows.  A call that has no
+// more than kAllFew in all takes every window for one of few, and a single window is
+// of the kind that its call's rows say: a launch of a kind that has nothing to do costs
+// 4 us (7 x 6 rows of 8B: 24 us without, 29 with).  64 rows of 8B over 16000 positions, 256
+// queries: 55 us as few rows, 43 as many.
+constexpr int kFewQueries = 64, kAllFew = 256;
 Classes classes_of(const PageArgs& pg, int rows, int nq, bool bf16) {
   const long long queries = (long long)rows * (nq / pg.nkv);
   Classes c{};
-  c.use_many = queries > (pg.n_windows > 1 ? 256 : 64);
+  c.use_many = queries > (pg.n_windows > 1 ? kAllFew : kFewQueries);
   c.use_few = !c.use_many || pg.n_windows > 1;
   c.few.qlo = 1;
-  c.few.qhi = c.use_many ? 64 : INT_MAX;
+  c.few.qhi = c.use_many ? kFewQueries : INT_MAX;
   c.few.once = kSlots;
+  // items of 1024 keys are long enough to hide how they begin and end, and what is cut
+  // finer than one for each workgroup evens out: 8B, 32 windows of up to 31131 positions,
+  // 512 items 404 us, 2048 353, 4096 361; 12 windows of 1 or 8 rows over up to 30000:
+  // items of 8 units 68 us, of 4 73, of 16 78
   c.few.most = 4 * kSlots;
   c.few.enough = 8;
-  c.many.qlo = c.use_few ? 65 : 1;
+  c.many.qlo = c.use_few ? kFewQueries + 1 : 1;
   c.many.qhi = INT_MAX;
   c.many.qw = 4;
   c.many.once = c.many.most = 4 * (many_two(pg.kvb, pg.hd, bf16) ? kSlots : kSlots / 2);

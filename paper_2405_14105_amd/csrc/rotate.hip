@@ -14,6 +14,10 @@
 // A row's sines are made once a wave, one pair a lane, and the lanes read those of
 // their pairs from LDS.  p f is formed in fp64 in turns and reduced there; what is
 // left, at most half a turn, is rounded to fp32 (2^-24 of it) and goes to sincospi.
+// 2048 rows of 8B: fp32 (84 MB) 13.9 us, 6 TB/s; bf16 12, with norms 14, where what a
+// wave does once (its row's position, sines, first loads) is most of it.  A workgroup
+// for a row, its sines made by one wave: 14 and 16.  8 bytes a piece for bf16: 11.7
+// and 16.  Rows of a dim that fills no whole pieces, entry by entry: 23 us instead of 14.
 // Values of a page lie [dim][32 positions]: 32 positions of a head are turned
 // over in LDS so that full runs of 8 positions leave as 16 bytes; a step of one
 // row writes 2 bytes into each dim's run, as the layout has it.
