@@ -478,7 +478,8 @@ constexpr int kMaxStepRows = 1 << 22;
 constexpr int kMaxStepHeads = 1024;
 constexpr int kMaxStepPositions = 1 << 30;
 constexpr int kMaxStepQueries = 1 << 28;   // of a KV head
-constexpr long long kMaxStepLd = 1ll << 40;
+constexpr long long kMaxStepLd = 1ll << 36;
+constexpr long long kMaxStepEntries = 1ll << 40;
 constexpr int kMaxBias = 1024;          // dsi_adjust: entries of a window's biases,
 constexpr int kMaxCount = 1 << 21;      // and tokens that a row has seen
 // A layer of a cache in pages and the rows of a step (rotate.hip, pages.hip):
@@ -535,6 +536,7 @@ struct PageClass {
   // long as an item then has no more than `enough` units of keys, up to `most`
   int once, most, enough;
   double inv_once, inv_most;
+  int* plan;            // nullable: the cut of more than 64 windows, written by a launch before
   int slots;            // of a KV head, for the parts of tiles that are cut
   float* part;          // [slots][nkv][32][head_dim]
   float2* ml;           // [slots][nkv][32]: maximum (base 2) and sum

@@ -22,37 +22,57 @@ __device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readl
 
 // The window that holds item t, windows contributing count(b) items each, and
 // the item's number within it; -1 if there are not that many.  Every lane of
-// the wave calls it with the same t.
+// the wave calls it with the same t.  Four windows a lane, whose loads are in
+// flight together.
 template <typename F>
 __device__ __forceinline__ int find_item(int n_windows, int t, F&& count, int& rest) {
   const int lane = threadIdx.x & 63;
-  for (int b0 = 0; b0 < n_windows; b0 += 64) {
-    const int c = b0 + lane < n_windows ? count(b0 + lane) : 0;
-    const int incl = wave_scan_incl(c);
+  for (int b0 = 0; b0 < n_windows; b0 += 256) {
+    int c[4], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int b = b0 + lane * 4 + i;
+      c[i] = b < n_windows ? count(b) : 0;
+      sum += c[i];
+    }
+    const int incl = wave_scan_incl(sum);
     const unsigned long long over = __ballot(incl > t);
     if (over) {
       const int l = __ffsll((long long)over) - 1;
-      rest = t - __builtin_amdgcn_readlane(incl - c, l);
-      return b0 + l;
+      rest = t - __builtin_amdgcn_readlane(incl - sum, l);
+      int b = b0 + l * 4;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const int n = __builtin_amdgcn_readlane(c[i], l);
+        if (b != b0 + l * 4 + i || rest < n) continue;
+        rest -= n;
+        ++b;
+      }
+      return b;
     }
     t -= __builtin_amdgcn_readlane(incl, 63);
   }
   return -1;
 }
-// the window of row r, or -1
+// the window of row r, or -1: the last of 64 runs of windows that begins no later,
+// and its windows
 __device__ __forceinline__ int window_of_row(const PageArgs& p, int rows, int r) {
-  const int lane = threadIdx.x & 63;
-  for (int b0 = 0; b0 < p.n_windows; b0 += 64) {
-    bool in = false;
-    if (b0 + lane < p.n_windows) {
-      int r0, r1;
-      window_rows(p, rows, b0 + lane, r0, r1);
-      in = r >= r0 && r < r1;
-    }
-    const unsigned long long m = __ballot(in);
-    if (m) return b0 + __ffsll((long long)m) - 1;
+  const int lane = threadIdx.x & 63, n = p.n_windows, run = (n + 63) >> 6;
+  int b0 = 0;
+  if (run > 1) {
+    const unsigned long long m = __ballot(lane * run < n && p.row0[min(lane * run, n)] <= r);
+    if (!m) return -1;
+    b0 = (63 - __clzll((long long)m)) * run;
   }
-  return -1;
+  const int b = b0 + lane;
+  bool in = false;
+  if (lane < (run > 1 ? run : 64) && b < n) {
+    int r0, r1;
+    window_rows(p, rows, b, r0, r1);
+    in = r >= r0 && r < r1;
+  }
+  const unsigned long long m = __ballot(in);
+  return m ? b0 + __ffsll((long long)m) - 1 : -1;
 }
 // the pool's index of the block that holds a window's positions [32 kb, 32 kb + 32)
 // of a KV head, or -1 without a page

@@ -68,15 +68,14 @@ __device__ __forceinline__ Win window_at(const PageAttnArgs& a, const PageClass&
   w.units = (span + kUnit - 1) / kUnit;
   return w;
 }
-// How a class is cut, as every lane of every wave works it out: units of an item at
-// most, and of the lane's window (the first 64) its items, or with JOIN the groups of
-// 32 queries of its tiles that are cut, and the slots of their parts, with those of
-// the lanes before.
+// How a class is cut: units of an item at most, and all items, or with JOIN the groups
+// of 32 queries of tiles that are cut.  Up to 64 windows every lane of every wave works
+// it out, a window a lane: the window's items, and the slots of their parts, with those
+// of the lanes before.  For more windows a launch of its own has written it down.
 struct Plan {
   Win w;
-  int per;
+  int per, total;
   int n, incl, split, sincl;
-  int total;            // of all windows, where there are no more than 64
 };
 // chunks of a tile: the last one may be a quarter longer than the others
 __device__ __forceinline__ int chunks_of(int units, int per) {
@@ -90,24 +89,26 @@ __device__ __forceinline__ void count(Plan& p) {
   p.incl = wave_scan_incl(p.n);
   p.sincl = wave_scan_incl(p.split);
 }
+// one item for each workgroup that the card holds where that leaves items short,
+// more of them, at most `most`, where they would be long
+__device__ __forceinline__ int units_per_item(const PageClass& cl, double work, bool& once_enough) {
+  const double once = ceil(work * cl.inv_once), fine = ceil(work * cl.inv_most);
+  once_enough = once <= cl.enough;
+  return (int)fmin(fmax(fmax(fine, fmin(once, (double)cl.enough)), 1.0), 1e9);
+}
 template <bool JOIN>
 __device__ __forceinline__ Plan plan_of(const PageAttnArgs& a, const PageClass& cl) {
-  const int lane = threadIdx.x & 63;
-  const bool whole = a.pg.n_windows <= 64;
   Plan p;
-  p.w = window_at(a, cl, lane);
-  double work = (double)(p.w.tiles * p.w.qw) * p.w.units;
-  for (int b = lane + 64; b < a.pg.n_windows; b += 64) {
-    const Win w = window_at(a, cl, b);
-    work += (double)(w.tiles * w.qw) * w.units;
+  if (cl.plan) {
+    p.per = cl.plan[0];
+    p.total = cl.plan[JOIN ? 2 : 1];
+    return p;
   }
-  work = wave_sum(work) * a.pg.nkv;
-  // one item for each workgroup that the card holds where that leaves items short,
-  // more of them, at most `most`, where they would be long
-  const double once = ceil(work * cl.inv_once), fine = ceil(work * cl.inv_most);
-  p.per = (int)fmin(fmax(fmax(fine, fmin(once, (double)cl.enough)), 1.0), 1e9);
+  p.w = window_at(a, cl, threadIdx.x & 63);
+  bool once_enough;
+  p.per = units_per_item(cl, wave_sum((double)(p.w.tiles * p.w.qw) * p.w.units) * a.pg.nkv, once_enough);
   // chunks are whole: a few units more where they are a few items too many for one turn
-  if (whole && once <= cl.enough && (long long)wave_total(p.w.tiles * p.w.qw) * a.pg.nkv <= cl.once) {
+  if (once_enough && (long long)wave_total(p.w.tiles * p.w.qw) * a.pg.nkv <= cl.once) {
     for (int i = 0; i < 6; ++i) {
       const int items = wave_total(p.w.tiles * p.w.qw * chunks_of(p.w.units, p.per));
       if ((long long)items * a.pg.nkv <= cl.once) break;
@@ -115,8 +116,61 @@ __device__ __forceinline__ Plan plan_of(const PageAttnArgs& a, const PageClass& 
     }
   }
   count<JOIN>(p);
-  p.total = whole ? __builtin_amdgcn_readlane(p.incl, 63) : INT_MAX;
+  p.total = __builtin_amdgcn_readlane(p.incl, 63);
   return p;
+}
+// The cut of more than 64 windows, a workgroup a class: units of an item, items, groups
+// of 32 queries to join; then items, groups and slots of the windows up to and with each
+constexpr int kPlanHead = 4, kPlanWindows = 4;   // windows a thread
+__global__ __launch_bounds__(1024) void k_page_plan(PageAttnArgs a, PageClass few, PageClass many, int first) {
+  __shared__ double works[16];
+  __shared__ int sums[3][16];
+  const PageClass& cl = (int)blockIdx.x + first ? many : few;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  Win win[kPlanWindows];
+  double work = 0.0;
+#pragma unroll
+  for (int i = 0; i < kPlanWindows; ++i) {
+    win[i] = window_at(a, cl, threadIdx.x * kPlanWindows + i);
+    work += (double)(win[i].tiles * win[i].qw) * win[i].units;
+  }
+  work = wave_sum(work);
+  if (lane == 0) works[w] = work;
+  __syncthreads();
+  work = 0.0;
+  for (int i = 0; i < 16; ++i) work += works[i];
+  bool once_enough;
+  const int per = units_per_item(cl, work * a.pg.nkv, once_enough);
+  int v[3][kPlanWindows], before[3] = {0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < kPlanWindows; ++i) {
+    const int chunks = chunks_of(win[i].units, per), items = win[i].tiles * chunks;
+    v[0][i] = before[0] += items;
+    v[1][i] = before[1] += chunks > 1 ? win[i].tiles * win[i].qw : 0;
+    v[2][i] = before[2] += chunks > 1 ? items * win[i].qw : 0;
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const int incl = wave_scan_incl(before[k]);
+    if (lane == 63) sums[k][w] = incl;
+    before[k] = incl - before[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    int total = 0;
+    for (int i = 0; i < 16; ++i) {
+      if (i < w) before[k] += sums[k][i];
+      total += sums[k][i];
+    }
+#pragma unroll
+    for (int i = 0; i < kPlanWindows; ++i) {
+      const int b = threadIdx.x * kPlanWindows + i;
+      if (b < a.pg.n_windows) cl.plan[kPlanHead + k * a.pg.n_windows + b] = before[k] + v[k][i];
+    }
+    if (threadIdx.x == 0 && k < 2) cl.plan[1 + k] = total;
+  }
+  if (threadIdx.x == 0) cl.plan[0] = per;
 }
 // One item: chunk `chunk` of `chunks` of a tile; JOIN: the 32 queries `sub` of a
 // tile of several chunks
@@ -127,44 +181,45 @@ struct Item {
   int slot;             // of the tile's first 32 queries and chunk 0 (qw slots a chunk)
 };
 template <bool JOIN>
-__device__ __forceinline__ bool find(const PageAttnArgs& a, const PageClass& cl, const Plan& first, int t, Item& it) {
-  if (t >= first.total) return false;
+__device__ __forceinline__ bool find(const PageAttnArgs& a, const PageClass& cl, const Plan& p, int t, Item& it) {
+  if (t >= p.total) return false;
   const int lane = threadIdx.x & 63;
-  Plan p = first;
-  int slots = 0;
-  for (int b0 = 0; b0 < a.pg.n_windows; b0 += 64) {
-    if (b0) {
-      p.w = window_at(a, cl, b0 + lane);
-      count<JOIN>(p);
-    }
-    const unsigned long long over = __ballot(p.incl > t);
-    if (over) {
-      const int l = __ffsll((long long)over) - 1;
-      auto at = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
-      const int in = t - at(p.incl - p.n);
-      it.w = Win{at(p.w.r0), at(p.w.R), at(p.w.len), at(p.w.bad), at(p.w.tiles), at(p.w.qw), at(p.w.units)};
-      it.b = b0 + l;
-      it.chunks = chunks_of(it.w.units, p.per);
-      it.per = (unsigned)(it.w.units + it.chunks - 1) / (unsigned)it.chunks;
-      if (JOIN) {
-        it.tile = (unsigned)in / (unsigned)it.w.qw;
-        it.sub = in - it.tile * it.w.qw;
-        it.chunk = 0;
-      } else {
-        const int tile = (unsigned)in / (unsigned)it.chunks;
-        it.chunk = in - tile * it.chunks;
-        it.tile = it.w.tiles - 1 - tile;   // the longest first
-        it.sub = 0;
-      }
-      it.slot = slots + at(p.sincl - p.split) + it.tile * it.chunks * it.w.qw;
-      // rows of windows that overlap may need more than there are: no output (NaN)
-      if (it.chunks > 1 && it.slot + it.chunks * it.w.qw > cl.slots) it.w.bad = 1;
-      return true;
-    }
-    t -= __builtin_amdgcn_readlane(p.incl, 63);
-    slots += __builtin_amdgcn_readlane(p.sincl, 63);
+  auto at = [&](int v, int l) { return __builtin_amdgcn_readlane(v, l); };
+  int in, slot;         // the item's number in its window, slots of the windows before
+  if (cl.plan) {
+    const int n = a.pg.n_windows;
+    const int* upto = cl.plan + kPlanHead + (JOIN ? n : 0);
+    const int v = upto[min(lane * 64 + 63, n - 1)];
+    const int g = __ffsll((long long)__ballot(v > t)) - 1;
+    const int u = upto[min(g * 64 + lane, n - 1)];
+    const int l = __ffsll((long long)__ballot(u > t)) - 1;
+    it.b = g * 64 + l;
+    in = t - (l ? at(u, l - 1) : g ? at(v, g - 1) : 0);
+    slot = it.b ? cl.plan[kPlanHead + 2 * n + it.b - 1] : 0;
+    it.w = window_at(a, cl, it.b);
+  } else {
+    const int l = __ffsll((long long)__ballot(p.incl > t)) - 1;
+    it.b = l;
+    in = t - at(p.incl - p.n, l);
+    slot = at(p.sincl - p.split, l);
+    it.w = Win{at(p.w.r0, l), at(p.w.R, l), at(p.w.len, l), at(p.w.bad, l), at(p.w.tiles, l), at(p.w.qw, l), at(p.w.units, l)};
   }
-  return false;
+  it.chunks = chunks_of(it.w.units, p.per);
+  it.per = (unsigned)(it.w.units + it.chunks - 1) / (unsigned)it.chunks;
+  if (JOIN) {
+    it.tile = (unsigned)in / (unsigned)it.w.qw;
+    it.sub = in - it.tile * it.w.qw;
+    it.chunk = 0;
+  } else {
+    const int tile = (unsigned)in / (unsigned)it.chunks;
+    it.chunk = in - tile * it.chunks;
+    it.tile = it.w.tiles - 1 - tile;   // the longest first
+    it.sub = 0;
+  }
+  it.slot = slot + it.tile * it.chunks * it.w.qw;
+  // rows of windows that overlap may need more than there are: no output (NaN)
+  if (it.chunks > 1 && it.slot + it.chunks * it.w.qw > cl.slots) it.w.bad = 1;
+  return true;
 }
 // positions of the first and the last row of queries [x0, x0 + n) of a window,
 // and the positions [lo, hi) that they see, lo the first of its block
@@ -968,10 +1023,30 @@ Classes classes_of(const PageArgs& pg, int rows, int nq, bool bf16) {
   return c;
 }
 
+// of a class's written cut
+size_t plan_bytes(const PageArgs& pg) {
+  return pg.n_windows > 64 ? (((size_t)kPlanHead + 3 * pg.n_windows) * sizeof(int) + 15) & ~(size_t)15 : 0;
+}
+
 template <bool KVB, int HD, bool QB>
 hipError_t launch_all(PageAttnArgs a, void* ws, hipStream_t s) {
   Classes c = classes_of(a.pg, a.rows, a.nq, QB);
+  const bool both = many_two(KVB, HD, QB) && c.use_few && c.use_many;   // in one launch
+  if (both) {
+    c.few.once = kSlots / 2;
+    c.few.inv_once = 1.0 / c.few.once;
+  }
   char* at = (char*)ws;
+  const size_t planned = plan_bytes(a.pg);
+  if (planned) {
+    c.few.plan = (int*)at;
+    c.many.plan = (int*)(at + planned);
+    at += 2 * planned;
+    const int first = c.use_few ? 0 : 1, classes = c.use_few + c.use_many;
+    hipLaunchKernelGGL(k_page_plan, dim3(classes), dim3(1024), 0, s, a, c.few, c.many, first);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   for (PageClass* cl : {&c.few, &c.many}) {
     if (cl == &c.few ? !c.use_few : !c.use_many) continue;
     const long long n = slots(*cl, a.pg, a.rows, a.nq);
@@ -994,13 +1069,9 @@ hipError_t launch_all(PageAttnArgs a, void* ws, hipStream_t s) {
     jmany = std::min(tiles * 4, (long long)c.many.most / nkv + 1);
   }
   if (nmany > INT_MAX) return hipErrorInvalidValue;
-  bool both = false;
   if constexpr (many_two(KVB, HD, QB)) {
-    both = nfew && nmany;
     if (both) {
       nfew = std::min(nfew, (long long)kSlots / 2);
-      c.few.once = kSlots / 2;
-      c.few.inv_once = 1.0 / c.few.once;
       hipLaunchKernelGGL((k_page_both<KVB, HD, QB>), dim3((unsigned)(nfew + nmany)), dim3(256), 0, s, a, c.few, c.many, (int)nfew);
     }
   }
@@ -1034,7 +1105,7 @@ size_t page_attend_workspace_bytes(const PageArgs& pg, int rows, int nq) {
     const Classes c = classes_of(pg, rows, nq, bf16);
     most = std::max(most, (size_t)((c.use_few ? slots(c.few, pg, rows, nq) : 0) + (c.use_many ? slots(c.many, pg, rows, nq) : 0)));
   }
-  return most * 32 * (pg.hd * sizeof(float) + sizeof(float2));
+  return 2 * plan_bytes(pg) + most * 32 * (pg.hd * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_page_attend(const PageAttnArgs& a, void* ws, hipStream_t s) {

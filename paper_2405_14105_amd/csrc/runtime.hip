@@ -2384,7 +2384,8 @@ dsi_status dsi_adjust(void* stream, const dsi_adjust_args* a) {
     return fail(DSI_EINVAL, "ld_seen must be positive, ld_seen + rows below %d", kMaxCount);
   if (a->rows >= kMaxCount) return fail(DSI_EINVAL, "rows must be below %d", kMaxCount);
   if (!a->n_windows || !a->rows) return DSI_OK;
-  if ((long long)a->n_windows * a->rows * a->vocab > kMaxStepLd) return fail(DSI_EINVAL, "n_windows*rows*vocab exceeds %lld", kMaxStepLd);
+  if ((long long)a->n_windows * a->rows * a->vocab > kMaxStepEntries)
+    return fail(DSI_EINVAL, "n_windows*rows*vocab exceeds %lld", kMaxStepEntries);
   const size_t esz = a->dtype == DSI_BF16 ? 2 : 4;
   DSI_TRY(rows_ok("logits", a->d_logits, a->ld, a->vocab, esz));
   DSI_TRY(rows_ok("output", a->d_out, a->ld_out, a->vocab, esz));

@@ -106,12 +106,15 @@ def test_strides_and_scale():
     check(Step([4, 9], [33, 100], 2, 64, BF16, 32), 4, BF16, scale=0.03, ld=4 * 64 + 8)
 
 
-def test_many_windows():
-    B = 150
+@pytest.mark.parametrize("B,most,hq,act", [(64, 3, 4, F32), (65, 3, 4, F32), (150, 3, 4, BF16), (700, 2, 2, F32), (4096, 2, 1, F32), (300, 2, 2, BF16)])
+def test_many_windows(B, most, hq, act):
     g = torch.Generator().manual_seed(3)
-    rows = torch.randint(0, 3, (B,), generator=g).tolist()
-    past = torch.randint(0, 200, (B,), generator=g).tolist()
-    check(Step(rows, past, 1, 32, BF16, 32), 4, F32)
+    rows = torch.randint(0, most, (B,), generator=g).tolist()
+    past = torch.randint(0, 100 if B > 300 else 300, (B,), generator=g).tolist()
+    if B < 4096:
+        rows[B // 2], past[B // 2] = 90, 1500     # one of many rows, cut as well
+        past[B - 1], rows[B - 1] = 2000, 1
+    check(Step(rows, past, 1, 32, BF16, 32), hq, act)
 
 
 @pytest.mark.parametrize("act,kv", [(F32, F32), (F32, BF16), (BF16, BF16)])

@@ -176,6 +176,26 @@ def test_append(act, kv, style, hd, dim, norm):
     assert (out[:step.before] == 7).all() and (out[r0:] == 7).all()
 
 
+@pytest.mark.parametrize("B", [64, 65, 130, 257, 1000, 4096])
+def test_append_to_many_windows(B):
+    hd = 32
+    g = torch.Generator().manual_seed(B)
+    rows = torch.randint(0, 3, (B,), generator=g).tolist()
+    rows[B // 3] = 70
+    past = torch.randint(0, 70, (B,), generator=g).tolist()
+    step = Step(rows, past, 1, hd, BF16, 32, before=1, behind=2).to("cuda")
+    x = rows_of(step.n, 1, hd, BF16, 5)
+    out = append(step, x, x, x, 1, []).cpu()
+    x, r0 = x.cpu(), step.before
+    assert torch.equal(out[1:-2], x[1:-2]) and (out[:1] == 7).all() and (out[-2:] == 7).all()
+    k, v, table = step.k.cpu(), step.v.cpu(), step.table.cpu().long()
+    for b, n in enumerate(rows):
+        at = torch.arange(past[b], past[b] + n)
+        page, place = table[b][at // 32], at % 32
+        assert torch.equal(k[page, 0, 0, 0, place], x[r0:r0 + n]) and torch.equal(v[page, 0, 0, :, place], x[r0:r0 + n])
+        r0 += n
+
+
 def test_append_without_queries_and_by_positions_of_its_own():
     """A token tree's rows: slots after each other, rotated by their depths."""
     hd, hkv = 64, 2

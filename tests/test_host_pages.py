@@ -134,6 +134,8 @@ def test_attend_refusals_and_workspace():
     slot = 32 * (64 * 4 + 8)
     assert dsi.dsi_page_attend_workspace(pages, 1 << 22, 4) == 2 * 2 * 2048 * slot
     assert dsi.dsi_page_attend_workspace(pages, 1, 4) == (1 + 1) * 2 * 4 * slot
+    crowd = dsi.make_pages(**{**PAGES, "n_windows": 65})   # whose cut is written down: 4 + 3 * 65 numbers a kind of windows
+    assert dsi.dsi_page_attend_workspace(crowd, 1 << 22, 4) == 2 * 2 * 2048 * slot + 2 * 800
     long = dsi.make_pages(**{**PAGES, "max_pages": 1 << 20})
     assert dsi.dsi_page_attend_workspace(long, 1, 4) == 2 * 2048 * slot
     # rows of the output may lie among those of the queries
