@@ -22,17 +22,24 @@ __device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readl
 
 // The window that holds item t, windows contributing count(b) items each, and
 // the item's number within it; -1 if there are not that many.  Every lane of
-// the wave calls it with the same t.  Four windows a lane, whose loads are in
-// flight together.
+// the wave calls it with the same t.  More than 64 windows: four a lane,
+// whose loads are in flight together.
 template <typename F>
 __device__ __forceinline__ int find_item(int n_windows, int t, F&& count, int& rest) {
   const int lane = threadIdx.x & 63;
+  if (n_windows <= 64) {
+    const int c = lane < n_windows ? count(lane) : 0, incl = wave_scan_incl(c);
+    const unsigned long long over = __ballot(incl > t);
+    const int l = __ffsll((long long)over) - 1;
+    if (over) rest = t - __builtin_amdgcn_readlane(incl - c, l);
+    return l;
+  }
   for (int b0 = 0; b0 < n_windows; b0 += 256) {
     int c[4], sum = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int b = b0 + lane * 4 + i;
-      c[i] = b < n_windows ? count(b) : 0;
+      const int b = b0 + lane * 4 + i, n = count(min(b, n_windows - 1));
+      c[i] = b < n_windows ? n : 0;
       sum += c[i];
     }
     const int incl = wave_scan_incl(sum);

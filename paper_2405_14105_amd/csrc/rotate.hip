@@ -20,7 +20,10 @@
 // and 16.  Rows of a dim that fills no whole pieces, entry by entry: 23 us instead of 14.
 // Values of a page lie [dim][32 positions]: 32 positions of a head are turned
 // over in LDS so that full runs of 8 positions leave as 16 bytes; a step of one
-// row writes 2 bytes into each dim's run, as the layout has it.
+// row writes 2 bytes into each dim's run, as the layout has it.  1024 windows of one row
+// (8B) take 57 us, most of it such blocks.  By the waves that take the rows' keys it
+// is 34, but the registers that this needs cost every call: 1026 rows of 13B 21.6 us
+// instead of 19, 42 rows of 8B 4.85 instead of 4.6.
 #include <algorithm>
 
 #include "pages.h"

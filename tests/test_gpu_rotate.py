@@ -146,7 +146,7 @@ def append(step, q, k, v, hq, freq, gain=1.0, style=0, gq=None, gk=None, pos=Non
 def test_append(act, kv, style, hd, dim, norm):
     """Rows of ragged windows enter their pages; everything else of the pool, and rows of no window, stay."""
     hq, hkv = 6, 3
-    step = Step([1, 0, 40, 7, 33], [95, 64, 20, 0, 31], hkv, hd, kv, 32, seed=hd, before=2, behind=3)
+    step = Step([1, 0, 40, 7, 33, 8, 9], [95, 64, 20, 0, 31, 28, 24], hkv, hd, kv, 32, seed=hd, before=2, behind=3)
     step.k.zero_()
     step.v.zero_()
     was_k, was_v = step.k.clone(), step.v.clone()
