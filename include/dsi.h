@@ -459,7 +459,8 @@ typedef struct {
  *   d_gain_q, _k   [head_dim] fp32, nullable: x is first divided by
  *                  sqrt(mean(x^2) + eps) over its head and multiplied by the gain
  *   d_q_out, d_k_out   [rows][ld_q_out], [rows][ld_k_out].  In place (the same
- *                  pointer and stride) or apart from the input
+ *                  pointer and stride) or apart from the input, and apart from
+ *                  the other's rows
  * No alignment beyond the type's.  rows = 0 does nothing. */
 typedef struct {
   int32_t rows, n_heads, n_kv_heads, head_dim, dtype;

@@ -2173,18 +2173,20 @@ static dsi_status rows_ok(const char* what, const void* p, int64_t ld, long long
     return fail(DSI_EINVAL, "%s: rows of %lld entries lie %lld apart", what, entries, (long long)ld);
   return DSI_OK;
 }
-// in place, or apart (columns of one buffer among others)
+// whether two buffers' rows share no byte (columns of one buffer among others)
+static bool rows_apart(const void* x, int64_t ld_x, long long nx, const void* y, int64_t ld_y, long long ny, int rows, size_t esz) {
+  const uintptr_t x0 = (uintptr_t)x, y0 = (uintptr_t)y;
+  const size_t bx = (size_t)nx * esz, by = (size_t)ny * esz, step = (size_t)ld_x * esz;
+  const uintptr_t x1 = x0 + (size_t)(rows - 1) * step + bx, y1 = y0 + (size_t)(rows - 1) * ld_y * esz + by;
+  if (x0 >= y1 || y0 >= x1) return true;
+  if (ld_x != ld_y) return false;
+  const size_t d = y0 >= x0 ? (y0 - x0) % step : (step - (x0 - y0) % step) % step;   // how far a row of y lies behind one of x
+  return d >= bx && d + by <= step;
+}
+// in place, or apart
 static dsi_status apart_ok(const char* what, const void* in, int64_t ld_in, const void* out, int64_t ld_out, int rows,
                            long long entries, size_t esz) {
-  if (in == out && ld_in == ld_out) return DSI_OK;
-  const uintptr_t i0 = (uintptr_t)in, o0 = (uintptr_t)out;
-  const size_t n = (size_t)entries * esz, step = (size_t)ld_in * esz;
-  const uintptr_t i1 = i0 + (size_t)(rows - 1) * step + n, o1 = o0 + (size_t)(rows - 1) * ld_out * esz + n;
-  if (i0 >= o1 || o0 >= i1) return DSI_OK;
-  if (ld_in == ld_out) {   // how far an output's row lies behind an input's
-    const size_t d = o0 >= i0 ? (o0 - i0) % step : (step - (i0 - o0) % step) % step;
-    if (d >= n && d + n <= step) return DSI_OK;
-  }
+  if ((in == out && ld_in == ld_out) || rows_apart(in, ld_in, entries, out, ld_out, entries, rows, esz)) return DSI_OK;
   return fail(DSI_EINVAL, "%s overlaps its output without being in place", what);
 }
 
@@ -2243,6 +2245,13 @@ dsi_status dsi_rotate(void* stream, const dsi_rotate_args* a) {
   };
   DSI_TRY(part("queries", a->n_heads, a->d_q, a->ld_q, a->d_q_out, a->ld_q_out));
   DSI_TRY(part("keys", a->n_kv_heads, a->d_k, a->ld_k, a->d_k_out, a->ld_k_out));
+  if (a->n_heads && a->n_kv_heads) {
+    const long long nq = (long long)a->n_heads * a->head_dim, nk = (long long)a->n_kv_heads * a->head_dim;
+    if (!rows_apart(a->d_q, a->ld_q, nq, a->d_k_out, a->ld_k_out, nk, a->rows, esz) ||
+        !rows_apart(a->d_k, a->ld_k, nk, a->d_q_out, a->ld_q_out, nq, a->rows, esz) ||
+        !rows_apart(a->d_q_out, a->ld_q_out, nq, a->d_k_out, a->ld_k_out, nk, a->rows, esz))
+      return fail(DSI_EINVAL, "an output of queries or keys overlaps the other's rows");
+  }
   r.q = a->d_q;
   r.k = a->d_k;
   r.qo = a->d_q_out;
@@ -2306,6 +2315,9 @@ dsi_status dsi_page_append(void* stream, const dsi_pages* pages, const dsi_page_
   }
   DSI_TRY(rows_ok("keys", a->d_k, a->ld_k, nk, esz));
   DSI_TRY(rows_ok("values", a->d_v, a->ld_v, nk, esz));
+  if (a->n_heads && (!rows_apart(a->d_k, a->ld_k, nk, a->d_q_out, a->ld_q_out, nq, a->rows, esz) ||
+                     !rows_apart(a->d_v, a->ld_v, nk, a->d_q_out, a->ld_q_out, nq, a->rows, esz)))
+    return fail(DSI_EINVAL, "the output of queries overlaps the keys or values");
   r.nv = r.nk;
   r.q = a->d_q;
   r.k = a->d_k;

@@ -168,3 +168,24 @@ def test_adjust_refusals(stub):
     assert grid(7, 6, 128256) == 7 * 32 * 3
     assert not hip.stub_mallocs()
     ''')
+
+
+def test_outputs_apart_from_the_other_rows(stub):
+    """The parts of one fused row (queries, keys, values), and what overlaps them."""
+    at = 1 << 20
+    ok = dict(stream=0, rows=5, n_heads=4, n_kv_heads=2, head_dim=64, d_q=at, d_k=at + 1024, d_pos=P, d_q_out=at, d_k_out=at + 1024,
+              rope=dsi.make_rope(64, P), ld_q=512, ld_k=512, ld_q_out=512, ld_k_out=512)
+    refused(dsi.dsi_rotate, ok, dict(d_q_out=at + 1024), dict(d_q_out=2 << 20, d_k_out=at), dict(d_q_out=2 << 20, d_k_out=2 << 20),
+            dict(d_q_out=at + 1536 + 1024), dict(d_q_out=2 << 20, d_k_out=(2 << 20) + 1020),
+            dict(d_q_out=2 << 20, ld_q_out=256, d_k_out=(2 << 20) + 1024))
+    pages = dsi.make_pages(2, 64, dsi.DSI_BF16, 8, 32, P, 2 * P, 1, 4, 3 * P, 4 * P, 5 * P)
+    ok = dict(stream=0, pages=pages, rows=5, n_heads=4, d_q=at, d_k=at + 1024, d_v=at + 1536, d_q_out=at, rope=dsi.make_rope(64, P),
+              ld_q=512, ld_k=512, ld_v=512, ld_q_out=512)
+    refused(dsi.dsi_page_append, ok, dict(d_q_out=at + 1024), dict(d_q=2 << 20, d_q_out=at + 512), dict(d_q=2 << 20, d_q_out=at + 1536, ld_q_out=640))
+    run(stub, '''
+    rope = dsi.make_rope(64, 4096)
+    at = 1 << 20
+    hip.stub_clear()
+    dsi.dsi_rotate(0, 5, 4, 2, 64, at, at + 1024, 4096, at, at + 1024, rope, ld_q=512, ld_k=512, ld_q_out=512, ld_k_out=512)
+    dsi.dsi_rotate(0, 1, 4, 2, 64, at, at + 1024, 4096, at + 2048, at + 3072, rope)
+    ''')
