@@ -187,5 +187,5 @@ def test_outputs_apart_from_the_other_rows(stub):
     at = 1 << 20
     hip.stub_clear()
     dsi.dsi_rotate(0, 5, 4, 2, 64, at, at + 1024, 4096, at, at + 1024, rope, ld_q=512, ld_k=512, ld_q_out=512, ld_k_out=512)
-    dsi.dsi_rotate(0, 1, 4, 2, 64, at, at + 1024, 4096, at + 2048, at + 3072, rope)
+    dsi.dsi_rotate(0, 1, 4, 2, 64, at, at + 1024, 4096, at + 4096, at + 8192, rope)
     ''')
