@@ -545,9 +545,8 @@ dsi_status dsi_page_append(void* stream, const dsi_pages* pages, const dsi_page_
  * whatever they hold, and pages that lie before every row's reach are not looked
  * up.  Numerics: fp32 scores, softmax statistics and sums.  fp32 queries over a
  * bf16 cache enter their products in three bf16 parts, probabilities too: fp32
- * throughout.  bf16 queries: a probability is rounded to bf16 where a window has
- * many rows, which doubles the output's own rounding error (2^-8 each), and to
- * two bf16 parts where it has few.  A key or value that is not finite reaches only
+ * throughout.  bf16 queries over one: a probability is two bf16 parts, 2^-16 of
+ * it left (an output's own rounding: 2^-8).  A key or value that is not finite reaches only
  * the rows that see it; an infinite one may give NaN there where the formula
  * gives a number or an infinity. */
 typedef struct {

@@ -643,15 +643,18 @@ __device__ __forceinline__ void few_item(const PageAttnArgs& a, const PageClass&
 // them the same stages of KS blocks of 32 keys, which go through LDS in fragment
 // order, the next one's on their way while one is worked on.  Queries stay in
 // registers.  Bound by the matrix cores, the fragment reads from LDS and the
-// exponentials: 8B, 2048 rows after 30000 positions 1.10 ms, 0.95 PFLOP/s, where a
-// large library product reaches 1.14.  (Fragments from memory to registers, each wave
-// its own: 1.88 ms.  Eight waves and stages through registers: 1.28.  Four waves that
-// way: 2.87, out of registers.)  A wave's loads of its queries have to be waited for
+// exponentials: 8B, 2048 rows after 30000 positions 1.44 ms, 0.72 PFLOP/s of the
+// formula's products and 1.08 of those done (the second one twice), where a large
+// library product reaches 1.14.  (All with one part, 1.10: fragments from memory to
+// registers, each wave its own: 1.88 ms.  Eight waves and stages through registers:
+// 1.28.  Four waves that way: 2.87, out of registers.)  A wave's loads of its queries have to be waited for
 // before the loop: the compiler's wait for them in it would be one for the stage just
 // asked for.
-// The probabilities of bf16 queries are rounded to bf16 (2^-8, as the outputs are):
-// a second part would be half as many matrix instructions again, and what it saves
-// (outputs off by 2.0e-3 of their norm against 1.7e-3) is less than their own rounding.
+// A probability of bf16 queries is two bf16 parts, 2^-16 of it left, as where rows are
+// few: the call's rows, not what a caller asks for, say which kernel a row meets.  One
+// part is a third less matrix work (2048 rows at 30000: 1.07 ms instead of 1.44; 13B,
+// 512 + 7 rows: 138 us instead of 149), but its rounding, 2^-8, adds as much to the
+// outputs as their own (off by 2.0e-3 of their norm in all, two parts 1.7e-3).
 template <bool KVB, int HD>
 struct ManyShared {
   static constexpr int KS = KVB ? 2 : 1, FP = KVB ? 1 : 2, DS = HD / 16, DT = HD / 32;
@@ -666,7 +669,7 @@ __device__ __forceinline__ void load_lds(const void* from, uint32_t off, uint32_
 }
 template <bool KVB, int HD, bool QB>
 __device__ __forceinline__ void many_item(const PageAttnArgs& a, const PageClass& cl, int block, ManyShared<KVB, HD>& sh) {
-  constexpr int NW = 4, QT = KVB ? (QB ? 1 : 3) : 2, PT = KVB ? (QB ? 1 : 3) : 1;
+  constexpr int NW = 4, QT = KVB ? (QB ? 1 : 3) : 2, PT = KVB ? (QB ? 2 : 3) : 1;
   typedef ManyShared<KVB, HD> S;
   constexpr int KS = S::KS, FP = S::FP, DS = S::DS, DT = S::DT, FB = S::FB, FR = S::FR;
   static_assert(sizeof(S) <= 1 << 16, "offsets of 16 bits");

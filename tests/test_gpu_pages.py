@@ -287,3 +287,21 @@ def test_two_calls_at_once():
             dsi.dsi_page_attend(streams[i].cuda_stream, steps[i].pages(), steps[i].n, hq, qs[i], outs[i], ws[i], sizes[i])
     torch.cuda.synchronize()
     assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+@pytest.mark.parametrize("rows", [[1, 12, 3], [130], [97, 2, 0, 40]])
+@pytest.mark.parametrize("hd", [32, 64, 96, 128])
+@pytest.mark.parametrize("kv", [F32, BF16])
+def test_probabilities_of_bf16_queries_keep_two_parts(rows, hd, kv):
+    """However many rows there are.  What two bf16 parts leave of a probability is a half step of a half step, 2^-16
+    of it (an fp32 cache: nothing); the rest of the bound is fp32's and the output's own rounding.  Outputs near
+    zero, where that is little, are where a single part (2^-8 of the probabilities) would show."""
+    hq = 4
+    step = Step(rows, [300, 41, 90, 7][:len(rows)], 2, hd, kv, 64, seed=hd)
+    q = (torch.randn((step.n, hq * hd), generator=torch.Generator().manual_seed(6)) * 2).to(BF16)
+    ref, mass, big = attend64(step, q.view(step.n, hq, hd), hq)
+    step.to("cuda")
+    got = attend(step, q.cuda(), hq).cpu().view(step.n, hq, hd).double()
+    tol = tolerance(step, ref, mass, big, F32) + (ref.abs() * HALF_STEP[BF16]) + (mass * 2.0 ** -16 if kv == BF16 else 0)
+    err = (got - ref).abs()
+    assert (err <= tol * (1 + HALF_STEP[BF16])).all(), ((err / tol).max(), err.max())
