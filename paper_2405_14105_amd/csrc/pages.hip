@@ -15,6 +15,7 @@
 // Windows of up to 64 queries of a KV head (few rows) are bound by reading the pages,
 // others by the matrix cores: two kernels, or one launch of both.
 #include <algorithm>
+#include <climits>
 #include <type_traits>
 
 #include "pages.h"
@@ -122,6 +123,10 @@ __device__ __forceinline__ Plan plan_of(const PageAttnArgs& a, const PageClass& 
 // The cut of more than 64 windows, a workgroup a class: units of an item, items, groups
 // of 32 queries to join; then items, groups and slots of the windows up to and with each
 constexpr int kPlanHead = 4, kPlanWindows = 4;   // windows a thread
+// Sums of items stop at the largest int (items of windows in order are far fewer: 2^28
+// queries are 2^21 tiles, and cuts add what the workspace holds).  Rows that thousands of
+// windows claim may have more; sums that wrapped would put items outside their windows.
+__device__ __forceinline__ int capped_sum(int a, int b) { return (int)min((unsigned)a + (unsigned)b, (unsigned)INT_MAX); }
 __global__ __launch_bounds__(1024) void k_page_plan(PageAttnArgs a, PageClass few, PageClass many, int first) {
   __shared__ double works[16];
   __shared__ int sums[3][16];
@@ -145,28 +150,30 @@ __global__ __launch_bounds__(1024) void k_page_plan(PageAttnArgs a, PageClass fe
 #pragma unroll
   for (int i = 0; i < kPlanWindows; ++i) {
     const int chunks = chunks_of(win[i].units, per), items = win[i].tiles * chunks;
-    v[0][i] = before[0] += items;
+    v[0][i] = before[0] = capped_sum(before[0], items);
     v[1][i] = before[1] += chunks > 1 ? win[i].tiles * win[i].qw : 0;
     v[2][i] = before[2] += chunks > 1 ? items * win[i].qw : 0;
   }
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
-    const int incl = wave_scan_incl(before[k]);
+    int incl = before[k];
+    dpp_steps([&](auto s) { incl = capped_sum(incl, dpp_from<decltype(s)::ctrl, decltype(s)::rows>(0, incl)); });
     if (lane == 63) sums[k][w] = incl;
-    before[k] = incl - before[k];
+    before[k] = __shfl_up(incl, 1);
+    if (lane == 0) before[k] = 0;
   }
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
     int total = 0;
     for (int i = 0; i < 16; ++i) {
-      if (i < w) before[k] += sums[k][i];
-      total += sums[k][i];
+      if (i < w) before[k] = capped_sum(before[k], sums[k][i]);
+      total = capped_sum(total, sums[k][i]);
     }
 #pragma unroll
     for (int i = 0; i < kPlanWindows; ++i) {
       const int b = threadIdx.x * kPlanWindows + i;
-      if (b < a.pg.n_windows) cl.plan[kPlanHead + k * a.pg.n_windows + b] = before[k] + v[k][i];
+      if (b < a.pg.n_windows) cl.plan[kPlanHead + k * a.pg.n_windows + b] = capped_sum(before[k], v[k][i]);
     }
     if (threadIdx.x == 0 && k < 2) cl.plan[1 + k] = total;
   }

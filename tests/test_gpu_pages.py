@@ -305,3 +305,20 @@ def test_probabilities_of_bf16_queries_keep_two_parts(rows, hd, kv):
     tol = tolerance(step, ref, mass, big, F32) + (ref.abs() * HALF_STEP[BF16]) + (mass * 2.0 ** -16 if kv == BF16 else 0)
     err = (got - ref).abs()
     assert (err <= tol * (1 + HALF_STEP[BF16])).all(), ((err / tol).max(), err.max())
+
+
+def test_rows_that_thousands_of_windows_claim():
+    """2048 windows that each claim 2^27 queries, more tiles of 128 than 31 bits count, and more rows than their tables hold."""
+    rows, hq, hd, B = 1 << 17, 1024, 32, 4096
+    k, v = (torch.zeros((1, 1, 1, *shape), dtype=BF16, device="cuda") for shape in ((1, 32, 32), (32, 32)))
+    table, lens = torch.zeros((B, 1), dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    row0 = torch.tensor([0, rows] * (B // 2) + [0], dtype=torch.int32, device="cuda")
+    pages = dsi.make_pages(1, hd, dsi.DSI_BF16, 1, 32, k, v, B, 1, table, lens, row0)
+    q = torch.zeros((rows, hq * hd), dtype=BF16, device="cuda")
+    out = torch.full((rows + 1, hq * hd), 7.0, dtype=BF16, device="cuda")
+    n = dsi.dsi_page_attend_workspace(pages, rows, hq)
+    ws = torch.full((n + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    dsi.dsi_page_attend(torch.cuda.current_stream().cuda_stream, pages, rows, hq, q, out, ws, n, dsi.DSI_BF16)
+    torch.cuda.synchronize()
+    assert (ws[n:] == 0xA5).all() and (out[rows] == 7).all()
+    assert all(x.isnan().all() for x in out[:rows].split(1 << 13))
