@@ -2392,7 +2392,7 @@ dsi_status dsi_adjust(void* stream, const dsi_adjust_args* a) {
   if (a->dtype != DSI_F32 && a->dtype != DSI_BF16) return fail(DSI_EINVAL, "bad dtype %d", a->dtype);
   if (a->n_bias < 0 || a->n_bias > kMaxBias) return fail(DSI_EINVAL, "n_bias must be in [0, %d]", kMaxBias);
   if (!a->d_seen != !a->d_n_seen) return fail(DSI_EINVAL, "d_seen and d_n_seen come together");
-  if (a->d_seen && (a->ld_seen < 1 || a->ld_seen + a->rows >= kMaxCount))
+  if (a->d_seen && (a->ld_seen < 1 || a->ld_seen >= kMaxCount - a->rows))
     return fail(DSI_EINVAL, "ld_seen must be positive, ld_seen + rows below %d", kMaxCount);
   if (a->rows >= kMaxCount) return fail(DSI_EINVAL, "rows must be below %d", kMaxCount);
   if (!a->n_windows || !a->rows) return DSI_OK;

@@ -189,3 +189,10 @@ def test_outputs_apart_from_the_other_rows(stub):
     dsi.dsi_rotate(0, 5, 4, 2, 64, at, at + 1024, 4096, at, at + 1024, rope, ld_q=512, ld_k=512, ld_q_out=512, ld_k_out=512)
     dsi.dsi_rotate(0, 1, 4, 2, 64, at, at + 1024, 4096, at + 4096, at + 8192, rope)
     ''')
+
+
+def test_adjust_refuses_lists_of_any_size_too_long():
+    """Lengths whose sum with the rows would pass 64 bits, and those just too long."""
+    ok = dict(stream=0, n_windows=2, rows=3, vocab=1000, d_logits=1 << 20, d_out=2 << 20, d_seen=P, d_n_seen=P, ld_seen=10)
+    refused(dsi.dsi_adjust, ok, dict(ld_seen=(1 << 63) - 1), dict(ld_seen=(1 << 63) - 3), dict(ld_seen=1 << 31), dict(ld_seen=(1 << 21) - 3),
+            dict(ld_seen=-(1 << 63)), dict(n_windows=1, rows=(1 << 22), ld_seen=1))
