@@ -536,7 +536,7 @@ dsi_status dsi_page_append(void* stream, const dsi_pages* pages, const dsi_page_
  *   dtype          of d_q and d_out (DSI_F32 or DSI_BF16)
  *   d_q, d_out     [rows][ld_q], [rows][ld_out], heads after each other, 16-byte
  *                  aligned rows; they do not overlap
- *   scale          0: 1 / sqrt(head_dim)
+ *   scale          0: 1 / sqrt(head_dim); times log2(e) still a finite fp32
  *   d_ws           at least dsi_page_attend_workspace bytes, 16-byte aligned, for
  *                  this call's work alone; what it holds does not matter
  * A window with a negative length, with rows beyond max_pages * page_size

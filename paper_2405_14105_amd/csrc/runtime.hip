@@ -1,6 +1,7 @@
 // Host runtime behind the C ABI: model and KV-cache objects, the launch plan
 // of one target forward over a batch of window rows, and the verification /
 // prefill / rollback entry points.
+#include <float.h>
 #include <limits.h>
 #include <math.h>
 #include <stdarg.h>
@@ -2355,7 +2356,9 @@ dsi_status dsi_page_attend(void* stream, const dsi_pages* pages, const dsi_page_
   DSI_TRY(page_attend_sizes_ok(pages, a->rows, a->n_heads, d.pg));
   if (a->dtype != DSI_F32 && a->dtype != DSI_BF16) return fail(DSI_EINVAL, "bad dtype %d", a->dtype);
   if (a->reach < 0) return fail(DSI_EINVAL, "reach must be >= 0");
-  if (!(a->scale >= 0.f) || !std::isfinite(a->scale)) return fail(DSI_EINVAL, "scale must be >= 0");
+  // the kernels' scores are to the base 2
+  d.scale2 = (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)pages->head_dim)) * 1.44269504088896340736f;
+  if (!(a->scale >= 0.f) || !std::isfinite(d.scale2)) return fail(DSI_EINVAL, "scale must be >= 0, at most %g", FLT_MAX / 1.4426950408889634);
   if (!a->rows) return DSI_OK;
   DSI_TRY(page_pointers_ok(pages));
   const size_t esz = a->dtype == DSI_BF16 ? 2 : 4;
@@ -2379,7 +2382,6 @@ dsi_status dsi_page_attend(void* stream, const dsi_pages* pages, const dsi_page_
   d.ldo = (size_t)a->ld_out;
   d.q = a->d_q;
   d.out = a->d_out;
-  d.scale2 = (a->scale > 0.f ? a->scale : 1.f / std::sqrt((float)pages->head_dim)) * 1.44269504088896340736f;
   HIP_TRY(launch_page_attend(d, a->d_ws, (hipStream_t)stream));
   return DSI_OK;
 }

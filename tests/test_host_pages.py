@@ -196,3 +196,14 @@ def test_adjust_refuses_lists_of_any_size_too_long():
     ok = dict(stream=0, n_windows=2, rows=3, vocab=1000, d_logits=1 << 20, d_out=2 << 20, d_seen=P, d_n_seen=P, ld_seen=10)
     refused(dsi.dsi_adjust, ok, dict(ld_seen=(1 << 63) - 1), dict(ld_seen=(1 << 63) - 3), dict(ld_seen=1 << 31), dict(ld_seen=(1 << 21) - 3),
             dict(ld_seen=-(1 << 63)), dict(n_windows=1, rows=(1 << 22), ld_seen=1))
+
+
+def test_attend_refuses_scales_that_are_infinite_to_the_base_2(stub):
+    """Scores are kept to the base 2: a scale times log2(e) has to be a number."""
+    ok = dict(stream=0, pages=dsi.make_pages(**PAGES), rows=5, n_heads=4, d_q=1 << 20, d_out=2 << 20, d_ws=3 << 20, ws_bytes=1 << 30)
+    refused(dsi.dsi_page_attend, ok, dict(scale=2.36e38), dict(scale=3.4e38), dict(scale=math.inf), dict(scale=-math.inf))
+    run(stub, '''
+    pages = dsi.make_pages(2, 64, dsi.DSI_BF16, 100, 64, 1 << 20, 2 << 20, 3, 8, P, P, P)
+    for scale in (0.0, 1e-45, 1.0, 2.35e38):
+        dsi.dsi_page_attend(0, pages, 5, 4, 1 << 20, 2 << 20, 3 << 20, 1 << 30, scale=scale)
+    ''')
