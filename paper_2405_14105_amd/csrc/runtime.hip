@@ -2305,6 +2305,7 @@ dsi_status dsi_page_append(void* stream, const dsi_pages* pages, const dsi_page_
   DSI_TRY(pages_ok(pages, r.pg));
   DSI_TRY(rotate_args(r, a->rows, a->n_heads, pages->n_kv_heads, pages->head_dim, a->dtype, a->d_pos, a->d_gain_q, a->d_gain_k,
                       a->eps, a->rope));
+  if ((long long)a->rows * r.nk > kMaxStepKeys) return fail(DSI_EINVAL, "rows * n_kv_heads exceeds %lld", kMaxStepKeys);
   if (!a->rows) return DSI_OK;
   DSI_TRY(page_pointers_ok(pages));
   const size_t esz = r.bf16 ? 2 : 4;
@@ -2339,6 +2340,7 @@ static dsi_status page_attend_sizes_ok(const dsi_pages* pages, int32_t rows, int
     return fail(DSI_EINVAL, "n_heads must be a multiple of n_kv_heads, at most %d", kMaxStepHeads);
   if ((long long)rows * (n_heads / p.nkv) > kMaxStepQueries)
     return fail(DSI_EINVAL, "rows * n_heads / n_kv_heads exceeds %d", kMaxStepQueries);
+  if ((long long)rows * n_heads > kMaxStepHeadRows) return fail(DSI_EINVAL, "rows * n_heads exceeds %lld", kMaxStepHeadRows);
   return DSI_OK;
 }
 
@@ -2400,6 +2402,8 @@ dsi_status dsi_adjust(void* stream, const dsi_adjust_args* a) {
   if (!a->n_windows || !a->rows) return DSI_OK;
   if ((long long)a->n_windows * a->rows * a->vocab > kMaxStepEntries)
     return fail(DSI_EINVAL, "n_windows*rows*vocab exceeds %lld", kMaxStepEntries);
+  if ((long long)a->n_windows * ((a->vocab - 1) / 4096 + 1) > kMaxStepChunks)
+    return fail(DSI_EINVAL, "n_windows * vocab / 4096 exceeds %d", kMaxStepChunks);
   const size_t esz = a->dtype == DSI_BF16 ? 2 : 4;
   DSI_TRY(rows_ok("logits", a->d_logits, a->ld, a->vocab, esz));
   DSI_TRY(rows_ok("output", a->d_out, a->ld_out, a->vocab, esz));
