@@ -286,3 +286,24 @@ def test_a_server_step_by_step(act, kv):
         tol = mass * (2 * big * off + 2.0 ** -17) + (ref.abs() + mass) * HALF_STEP[act]
         err = (got[b].double().view(n, hq, hd) - ref).abs()
         assert (err <= tol).all(), (err / tol).max()
+
+
+@pytest.mark.parametrize("style", STYLES)
+def test_sines_near_zero_keep_their_digits(style):
+    """Pairs (1, 0) become (cos, sin): to 2^-21 of the value each (two steps of 2^-23 of the sine, half a step of the sum), and
+    what fp64 leaves of the angle, three half steps of 2^-53.  An angle rounded to fp32 would be off by 2^-24 whatever the value."""
+    hd, n = 128, 4096
+    x = torch.zeros((n, hd))
+    x[:, :hd // 2] = 1.0
+    if style == dsi.DSI_ROPE_PAIRS:
+        x = x.view(n, 2, hd // 2).transpose(1, 2).reshape(n, hd).contiguous()
+    pos = torch.arange(n, dtype=torch.int32) * 37
+    freq = dsi.dsi_rope_table(hd)[0]
+    q, _ = rotate(x.cuda(), x.cuda().clone(), 1, 1, hd, pos, freq, 1.0, style)
+    got = q.cpu().double()
+    c, s = (got[:, :hd // 2], got[:, hd // 2:]) if style == dsi.DSI_ROPE_HALF else (got[:, 0::2], got[:, 1::2])
+    angle = torch.outer(pos.double(), torch.tensor(freq, dtype=torch.float64))
+    for y, ref in ((c, angle.cos()), (s, angle.sin())):
+        tol = ref.abs() * 2.0 ** -21 + angle.abs() * 2.0 ** -51 + 2.0 ** -46
+        err = (y - ref).abs()
+        assert (err <= tol).all(), (err / tol).max()
