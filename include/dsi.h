@@ -574,6 +574,10 @@ dsi_status dsi_page_attend(void* stream, const dsi_pages* pages, const dsi_page_
  *   z = z - frequency c - (c > 0 ? presence : 0)
  *   z = z + bias(v);  z = -inf where v is not allowed
  * so that every row of a verified window is judged by the text it continues.
+ * One count serves the three penalties.  Repetition over a prompt and its output
+ * with frequency and presence over the output alone takes two calls: repetition
+ * with the one list, then, in place, frequency, presence, biases and mask with the
+ * other.
  *   d_logits       [n_windows*rows][ld], d_out [n_windows*rows][ld_out], entries
  *                  of type dtype; in place (the same pointer and stride; only
  *                  what changes, and its neighbours within 16 bytes, is then

@@ -203,3 +203,20 @@ def test_verification_by_adjusted_logits():
                 k += 1
             assert int(n[b]) == k and int(tok[b]) == int(best[b, k])
         s["tokens"] = torch.randint(0, V, (B, R), generator=torch.Generator().manual_seed(turn + 2), dtype=torch.int32)
+
+
+def test_repetition_over_a_text_and_penalties_over_its_output_alone():
+    """Two calls, the second in place: one count serves the three penalties of a call."""
+    B, R, V = 3, 4, 5003
+    s = make(B, R, V, F32, n_bias=5, allowed=70, seed=2)
+    text, output = dict(s), dict(s)
+    text.update(freq=None, pres=None, mask=None, ids=torch.zeros((B, 0), dtype=torch.int32), bias=torch.zeros((B, 0)))
+    output.update(rep=None, seen=s["seen"][:, -9:].contiguous(), n_seen=torch.tensor([9, 0, 5], dtype=torch.int32))
+    first, tol = formula(text)
+    output["z"] = call(text)
+    got = call(output, True)
+    output["z"] = first
+    ref, more = formula(output)
+    inf = ref.isinf()
+    assert torch.equal(got.double()[inf], ref[inf])
+    assert ((got.double() - ref).abs() <= tol + more)[~inf].all()
