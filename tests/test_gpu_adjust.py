@@ -205,6 +205,22 @@ def test_verification_by_adjusted_logits():
         s["tokens"] = torch.randint(0, V, (B, R), generator=torch.Generator().manual_seed(turn + 2), dtype=torch.int32)
 
 
+@pytest.mark.parametrize("act", [F32, BF16])
+def test_entries_that_nothing_changes_are_not_written_in_place(act):
+    """bf16: a NaN whose quiet bit is clear would come back with it set from a run that is read, rounded and written."""
+    s = make(2, 3, 9001, act, n_bias=0, allowed=None, seen=2)
+    bits, pattern = (torch.int32, 0x7FA12345) if act == F32 else (torch.int16, 0x7FA1)
+    s["z"].view(bits)[:] = pattern
+    s["seen"][:], s["n_seen"][:], s["tokens"][:] = torch.tensor([17, 8999]), 2, 4100
+    got = call(s, True).view(bits)
+    run = 16 // s["z"].element_size()   # entries of 16 bytes
+    rest = torch.ones(9001, dtype=torch.bool)
+    for token in (17, 8999, 4100):
+        rest[token // run * run:token // run * run + run] = False
+    assert (got[:, rest] == pattern).all()
+    assert act == F32 or (got[:, 4101] != pattern).all()   # what the pattern shows where a run was written
+
+
 def test_repetition_over_a_text_and_penalties_over_its_output_alone():
     """Two calls, the second in place: one count serves the three penalties of a call."""
     B, R, V = 3, 4, 5003
