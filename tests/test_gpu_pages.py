@@ -322,3 +322,16 @@ def test_rows_that_thousands_of_windows_claim():
     torch.cuda.synchronize()
     assert (ws[n:] == 0xA5).all() and (out[rows] == 7).all()
     assert all(x.isnan().all() for x in out[:rows].split(1 << 13))
+
+
+@pytest.mark.parametrize("B,hkv,hq,hd,page,kv,act,reach", [
+    (65, 2, 8, 64, 64, BF16, F32, 0), (70, 8, 8, 128, 96, BF16, BF16, 0), (150, 2, 6, 96, 64, F32, F32, 0), (90, 8, 16, 64, 32, BF16, BF16, 100),
+    (130, 3, 3, 128, 64, F32, BF16, 333), (300, 2, 2, 32, 128, BF16, F32, 50)])
+def test_many_windows_of_several_kv_heads(B, hkv, hq, hd, page, kv, act, reach):
+    """More than 64 windows, whose cut is written down first: one of few rows and one of many are cut and joined."""
+    g = torch.Generator().manual_seed(B)
+    rows, past = torch.randint(0, 3, (B,), generator=g).tolist(), torch.randint(0, 120, (B,), generator=g).tolist()
+    rows[B // 3], past[B // 3] = 2, 3000
+    rows[B // 2], past[B // 2] = 300 * hkv // hq, 1200
+    rows[B - 1], past[B - 1] = 0, 5000
+    check(Step(rows, past, hkv, hd, kv, page, reach=reach, seed=B, before=1, behind=2), hq, act)

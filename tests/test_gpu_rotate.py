@@ -307,3 +307,29 @@ def test_sines_near_zero_keep_their_digits(style):
         tol = ref.abs() * 2.0 ** -21 + angle.abs() * 2.0 ** -51 + 2.0 ** -46
         err = (y - ref).abs()
         assert (err <= tol).all(), (err / tol).max()
+
+
+@pytest.mark.parametrize("B,hkv,hd,page,kv", [(65, 2, 64, 64, BF16), (130, 8, 128, 96, BF16), (300, 3, 96, 64, F32)])
+def test_append_to_many_windows_of_several_kv_heads(B, hkv, hd, page, kv):
+    g = torch.Generator().manual_seed(B)
+    rows, past = torch.randint(0, 3, (B,), generator=g).tolist(), torch.randint(0, 200, (B,), generator=g).tolist()
+    rows[B // 3], rows[B - 1] = 100, 40
+    step = Step(rows, past, hkv, hd, kv, page, before=1, behind=2).to("cuda")
+    step.k.zero_(), step.v.zero_()
+    k, v = rows_of(step.n, hkv, hd, BF16, 5), rows_of(step.n, hkv, hd, BF16, 6)
+    freq = dsi.dsi_rope_table(hd)[0]
+    out = append(step, k, k, v, hkv, freq).cpu().view(step.n, hkv, hd)
+    step.to("cpu")
+    k, v, r0 = k.cpu().view(step.n, hkv, hd), v.cpu().view(step.n, hkv, hd), step.before
+    new_k = new_v = 0
+    for b, n in enumerate(rows):
+        at = torch.arange(past[b], past[b] + n)
+        K, V = step.keys(b)
+        ref, mag = turned64(k[r0:r0 + n], at, freq, 1.0, 0)
+        close(K[past[b]:], ref, mag, hd, False, kv)
+        close(out[r0:r0 + n], ref, mag, hd, False, BF16)
+        assert torch.equal(V[past[b]:], v[r0:r0 + n].to(kv))
+        new_k, new_v = new_k + (K[past[b]:] != 0).sum(), new_v + (V[past[b]:] != 0).sum()
+        r0 += n
+    assert (out[:1] == 7).all() and (out[-2:] == 7).all()
+    assert (step.k != 0).sum() == new_k and (step.v != 0).sum() == new_v   # and nothing else
