@@ -516,7 +516,8 @@ typedef struct {
  *   d_q            nullable with d_q_out, n_heads then 0
  *   d_v            [rows][ld_v], heads after each other
  *   d_pos          [rows] int32, nullable: the positions rotated by, where they
- *                  are not those of the cache (a token tree's depths) */
+ *                  are not those of the cache.  (A token tree's depths would be
+ *                  such positions, but dsi_page_attend knows no tree.) */
 typedef struct {
   int32_t rows, n_heads, dtype;
   int64_t ld_q, ld_k, ld_v, ld_q_out;
@@ -536,7 +537,9 @@ dsi_status dsi_page_append(void* stream, const dsi_pages* pages, const dsi_page_
 /* Attention of a step's rows over their windows' pages, the rows' own keys and
  * values among them (dsi_page_append first): the row at position p of a window
  * sees [max(0, p - reach + 1), p], or [0, p] with reach = 0, query head h reads KV
- * head h / (n_heads / n_kv_heads), and out = softmax(scale q K^T) V.
+ * head h / (n_heads / n_kv_heads), and out = softmax(scale q K^T) V.  What a row
+ * sees goes by the cache's positions alone: rows of a token tree would see their
+ * siblings too, which only dsi_verify_tree keeps apart.
  *   dtype          of d_q and d_out (DSI_F32 or DSI_BF16)
  *   d_q, d_out     [rows][ld_q], [rows][ld_out], heads after each other, 16-byte
  *                  aligned rows; they do not overlap
@@ -550,9 +553,15 @@ dsi_status dsi_page_append(void* stream, const dsi_pages* pages, const dsi_page_
  * up.  Numerics: fp32 scores, softmax statistics and sums.  fp32 queries over a
  * bf16 cache enter their products in three bf16 parts, probabilities too: fp32
  * throughout.  bf16 queries over one: a probability is two bf16 parts, 2^-16 of
- * it left (an output's own rounding: 2^-8).  A key or value that is not finite reaches only
- * the rows that see it; an infinite one may give NaN there where the formula
- * gives a number or an infinity. */
+ * it left (an output's own rounding: 2^-8).  A key or value that is not finite
+ * reaches only the rows that see it; an infinite one may give NaN there where the
+ * formula gives a number or an infinity.  The same call gives the same bits.  Windows
+ * of few and of many rows meet different kernels, whose sums go in different
+ * orders.  Where a call declares several windows and more than 256 queries of a KV
+ * head (rows * n_heads / n_kv_heads), each window's rows on the device say which
+ * (few: up to 64 queries); otherwise all of them meet the one that the declared
+ * rows say (few: up to 256, of one window 64).  A call replayed for much less
+ * than it declares is right, but slower than one that declares it. */
 typedef struct {
   int32_t rows, n_heads, dtype, reach;
   int64_t ld_q, ld_out;
