@@ -854,7 +854,7 @@ __global__ __launch_bounds__(256, KVB || HD < 128 ? 2 : 1) void k_page_few(PageA
   few_items<KVB, HD, QB>(a, cl, blockIdx.x, gridDim.x, sh);
 }
 // Two workgroups fit a CU but where fp32 queries or keys of wide heads take more than
-// 256 registers.
+// 256 registers.  (bf16 ones of head dim 128 take all of them and 20 bytes of scratch a lane.)
 constexpr bool many_two(bool kvb, int hd, bool qb) { return hd <= 64 || (kvb && qb); }
 template <bool KVB, int HD, bool QB>
 __global__ __launch_bounds__(256, many_two(KVB, HD, QB) ? 2 : 1) void k_page_many(PageAttnArgs a, PageClass cl) {
@@ -864,8 +864,8 @@ __global__ __launch_bounds__(256, many_two(KVB, HD, QB) ? 2 : 1) void k_page_man
 
 // Both in one launch where two workgroups of either fit a CU: those for few rows come
 // first, one for each CU, and items of many rows beside them.  (1B, 500 rows beside
-// 15 single ones: 39 us one after the other, 33 together; 8B, 300 beside 8 x 6: 40 and
-// 28; 13B, 512 beside 7: 134 and 131, both bound by the memory by then.)
+// 15 single ones: 41 us one after the other, 36 together; 8B, 300 beside 8 x 6: 41 and
+// 28; 13B, 512 beside 7: 153 and 141, where both read much.)
 template <bool KVB, int HD, bool QB>
 __global__ __launch_bounds__(256, 2) void k_page_both(PageAttnArgs a, PageClass few, PageClass many, int nfew) {
   __shared__ union Both {
@@ -1005,7 +1005,7 @@ struct Classes {
 // more than kAllFew in all takes every window for one of few, and a single window is
 // of the kind that its call's rows say: a launch of a kind that has nothing to do costs
 // 4 us (7 x 6 rows of 8B: 24 us without, 29 with).  64 rows of 8B over 16000 positions, 256
-// queries: 55 us as few rows, 43 as many.
+// queries: 55 us as few rows, 46 as many.
 constexpr int kFewQueries = 64, kAllFew = 256;
 Classes classes_of(const PageArgs& pg, int rows, int nq, bool bf16) {
   const long long queries = (long long)rows * (nq / pg.nkv);

@@ -15,8 +15,11 @@
 // their pairs from LDS.  p f is formed in fp64 in turns and reduced there; what is
 // left, at most half a turn, goes to sincospi in fp32, and what that leaves of it turns
 // the result on: sines near zero keep their digits.
-// 2048 rows of 8B: fp32 (84 MB) 13.9 us, 6 TB/s; bf16 12, with norms 14, where what a
-// wave does once (its row's position, sines, first loads) is most of it.  A workgroup
+// 2048 rows of 8B: fp32 (84 MB) 13.6 us, 6.2 TB/s; bf16 (42 MB) 12, with norms 14, where
+// vector instructions are issued in 69 % of the busy cycles and a lane's sines go
+// through scratch (68 bytes a lane, 17 of the 38 MB written): four waves a SIMD leave
+// 128 registers, 139 are needed.  Three waves without scratch are no faster: 12, with
+// norms 15.6, 1026 rows of 13B 21.2 instead of 19.4.  A workgroup
 // for a row, its sines made by one wave: 14 and 16.  8 bytes a piece for bf16: 11.7
 // and 16.  Rows of a dim that fills no whole pieces, entry by entry: 23 us instead of 14.
 // Values of a page lie [dim][32 positions]: 32 positions of a head are turned
