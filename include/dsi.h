@@ -410,9 +410,11 @@ dsi_status dsi_logprobs(void* stream, const dsi_logprobs_args* args);
  * may be replayed with others; whatever they hold, no memory outside the
  * buffers that a call names is touched.
  * Sizes: rows (dsi_adjust: n_windows * rows) at most 2^22, heads 1024, rows from
- * one to the next 2^36 entries; an append rows * n_kv_heads 2^27; attention rows *
- * n_heads 2^30, of a KV head 2^28, a window 2^30 positions; adjustment n_windows *
- * vocab / 4096 (rounded up) 2^24 - 2^11, n_windows * rows * vocab 2^40. */
+ * one to the next 2^36 entries, a window 2^30 positions, queries of a KV head (rows
+ * * n_heads / n_kv_heads) 2^28, entries of logits 2^40; and what one launch holds,
+ * fewer than 2^24 workgroups: an append takes about n_kv_heads (rows / 32 + 2
+ * n_windows) of them, attention rows * n_heads / 128 + n_windows * n_kv_heads,
+ * adjustment n_windows * vocab / 4096.  Calls beyond are refused. */
 
 /* Which entries of a head a rotation turns together: HALF: j and j + dim/2;
  * PAIRS: 2j and 2j + 1. */

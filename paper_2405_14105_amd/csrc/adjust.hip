@@ -183,6 +183,7 @@ hipError_t launch_adjust(AdjustArgs a, hipStream_t s) {
   a.groups = (int)std::min((long long)a.R, (kAdjFull + each - 1) / each);
   a.rpg = (a.R + a.groups - 1) / a.groups;
   a.groups = (a.R + a.rpg - 1) / a.rpg;
+  if (each * a.groups > kMaxStepBlocks) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)(each * a.groups)), block(kAdjThreads);
   const bool place = a.z == a.out && a.ld == a.ldo;
   if (a.bf16) {

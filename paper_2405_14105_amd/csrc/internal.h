@@ -478,12 +478,10 @@ constexpr int kMaxStepRows = 1 << 22;
 constexpr int kMaxStepHeads = 1024;
 constexpr int kMaxStepPositions = 1 << 30;
 constexpr int kMaxStepQueries = 1 << 28;   // of a KV head
-// A launch has fewer than 2^32 threads, 2^24 workgroups of 256.  Rotation: 2^20 of queries
-// and keys.  Append: the blocks of values besides, n_kv_heads (2 n_windows + rows / 32) at
-// most, 2^23 + 2^22.  Attention: n_heads (n_windows + rows / 128) about, 2^22 + 2^23.
-constexpr long long kMaxStepKeys = 1ll << 27;      // rows * n_kv_heads of an append
-constexpr long long kMaxStepHeadRows = 1ll << 30;  // rows * n_heads of an attention
-constexpr int kMaxStepChunks = (1 << 24) - (1 << 11);   // of adjusted windows, 4096 entries each; rows add 2^10 at most
+// Workgroups of 256 threads in a launch: its threads are counted in 32 bits, and one of more
+// runs what its number leaves past 2^32 without an error.  Their launchers return
+// hipErrorInvalidConfiguration instead, and launch nothing.
+constexpr long long kMaxStepBlocks = (1 << 24) - 1;
 constexpr long long kMaxStepLd = 1ll << 36;
 constexpr long long kMaxStepEntries = 1ll << 40;
 constexpr int kMaxBias = 1024;          // dsi_adjust: entries of a window's biases,

@@ -1046,6 +1046,21 @@ hipError_t launch_all(PageAttnArgs a, void* ws, hipStream_t s) {
     c.few.once = kSlots / 2;
     c.few.inv_once = 1.0 / c.few.once;
   }
+  const int nkv = a.pg.nkv, windows = std::min(a.pg.n_windows, a.rows);
+  long long nfew = 0, nmany = 0, jfew = 0, jmany = 0;
+  if (c.use_few) {
+    const long long tiles = most_tiles(a.pg, a.rows, a.nq, 1), cuts = c.few.most / nkv + 1;
+    nfew = std::min((cuts + tiles) * nkv, (long long)kSlots);
+    // the last tile of a window may have 32 queries that are empty
+    jfew = std::min(tiles + windows, cuts);
+  }
+  if (c.use_many) {
+    const long long tiles = most_tiles(a.pg, a.rows, a.nq, 4);
+    nmany = (c.many.most / 4 / nkv + 1 + tiles) * nkv;
+    jmany = std::min(tiles * 4, (long long)c.many.most / nkv + 1);
+  }
+  if (both) nfew = std::min(nfew, (long long)kSlots / 2);
+  if (nmany + (both ? nfew : 0) > kMaxStepBlocks) return hipErrorInvalidConfiguration;
   char* at = (char*)ws;
   const size_t planned = plan_bytes(a.pg);
   if (planned) {
@@ -1065,25 +1080,9 @@ hipError_t launch_all(PageAttnArgs a, void* ws, hipStream_t s) {
     cl->part = (float*)(cl->ml + n * 32);
     at = (char*)(cl->part + n * 32 * HD);
   }
-  const int nkv = a.pg.nkv, windows = std::min(a.pg.n_windows, a.rows);
-  long long nfew = 0, nmany = 0, jfew = 0, jmany = 0;
-  if (c.use_few) {
-    const long long tiles = most_tiles(a.pg, a.rows, a.nq, 1), cuts = c.few.most / nkv + 1;
-    nfew = std::min((cuts + tiles) * nkv, (long long)kSlots);
-    // the last tile of a window may have 32 queries that are empty
-    jfew = std::min(tiles + windows, cuts);
-  }
-  if (c.use_many) {
-    const long long tiles = most_tiles(a.pg, a.rows, a.nq, 4);
-    nmany = (c.many.most / 4 / nkv + 1 + tiles) * nkv;
-    jmany = std::min(tiles * 4, (long long)c.many.most / nkv + 1);
-  }
-  if (nmany > INT_MAX) return hipErrorInvalidValue;
   if constexpr (many_two(KVB, HD, QB)) {
-    if (both) {
-      nfew = std::min(nfew, (long long)kSlots / 2);
+    if (both)
       hipLaunchKernelGGL((k_page_both<KVB, HD, QB>), dim3((unsigned)(nfew + nmany)), dim3(256), 0, s, a, c.few, c.many, (int)nfew);
-    }
   }
   if (nmany && !both) hipLaunchKernelGGL((k_page_many<KVB, HD, QB>), dim3((unsigned)nmany), dim3(256), 0, s, a, c.many);
   hipError_t e = hipGetLastError();

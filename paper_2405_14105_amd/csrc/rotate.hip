@@ -369,6 +369,7 @@ hipError_t launch(RotateArgs a, hipStream_t s) {
     values = (long long)a.pg.nkv * std::min((long long)a.rows, 2ll * n + (a.rows - n) / 32);
   }
   if (a.row_blocks + values < 1) return hipSuccess;
+  if (a.row_blocks + values > kMaxStepBlocks) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((k_rotate<T>), dim3((unsigned)(a.row_blocks + values)), dim3(kRotWaves * 64), 0, s, a);
   return hipGetLastError();
 }

@@ -2165,6 +2165,12 @@ dsi_status dsi_rope_table(const dsi_rope_spec* s, double* freq, float* gain) {
   return DSI_OK;
 }
 
+// launches of the calls on pages: sizes that no launch holds are the caller's
+static dsi_status launched(hipError_t e, const char* what) {
+  if (e == hipErrorInvalidConfiguration) return fail(DSI_EINVAL, "%s: more than %lld workgroups", what, kMaxStepBlocks);
+  return e == hipSuccess ? DSI_OK : fail(DSI_EHIP, "%s failed: %s", what, hipGetErrorString(e));
+}
+
 static bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 // rows of `heads` heads, ld entries apart
 static dsi_status rows_ok(const char* what, const void* p, int64_t ld, long long entries, size_t esz) {
@@ -2261,8 +2267,7 @@ dsi_status dsi_rotate(void* stream, const dsi_rotate_args* a) {
   r.ldk = (size_t)a->ld_k;
   r.ldqo = (size_t)a->ld_q_out;
   r.ldko = (size_t)a->ld_k_out;
-  HIP_TRY(launch_rotate(r, (hipStream_t)stream));
-  return DSI_OK;
+  return launched(launch_rotate(r, (hipStream_t)stream), "rotation");
 }
 
 static dsi_status pages_ok(const dsi_pages* p, PageArgs& o) {
@@ -2305,7 +2310,6 @@ dsi_status dsi_page_append(void* stream, const dsi_pages* pages, const dsi_page_
   DSI_TRY(pages_ok(pages, r.pg));
   DSI_TRY(rotate_args(r, a->rows, a->n_heads, pages->n_kv_heads, pages->head_dim, a->dtype, a->d_pos, a->d_gain_q, a->d_gain_k,
                       a->eps, a->rope));
-  if ((long long)a->rows * r.nk > kMaxStepKeys) return fail(DSI_EINVAL, "rows * n_kv_heads exceeds %lld", kMaxStepKeys);
   if (!a->rows) return DSI_OK;
   DSI_TRY(page_pointers_ok(pages));
   const size_t esz = r.bf16 ? 2 : 4;
@@ -2328,8 +2332,7 @@ dsi_status dsi_page_append(void* stream, const dsi_pages* pages, const dsi_page_
   r.ldk = (size_t)a->ld_k;
   r.ldv = (size_t)a->ld_v;
   r.ldqo = (size_t)a->ld_q_out;
-  HIP_TRY(launch_rotate(r, (hipStream_t)stream));
-  return DSI_OK;
+  return launched(launch_rotate(r, (hipStream_t)stream), "append");
 }
 
 static dsi_status page_attend_sizes_ok(const dsi_pages* pages, int32_t rows, int32_t n_heads, PageArgs& p) {
@@ -2339,7 +2342,6 @@ static dsi_status page_attend_sizes_ok(const dsi_pages* pages, int32_t rows, int
     return fail(DSI_EINVAL, "n_heads must be a multiple of n_kv_heads, at most %d", kMaxStepHeads);
   if ((long long)rows * (n_heads / p.nkv) > kMaxStepQueries)
     return fail(DSI_EINVAL, "rows * n_heads / n_kv_heads exceeds %d", kMaxStepQueries);
-  if ((long long)rows * n_heads > kMaxStepHeadRows) return fail(DSI_EINVAL, "rows * n_heads exceeds %lld", kMaxStepHeadRows);
   return DSI_OK;
 }
 
@@ -2383,8 +2385,7 @@ dsi_status dsi_page_attend(void* stream, const dsi_pages* pages, const dsi_page_
   d.ldo = (size_t)a->ld_out;
   d.q = a->d_q;
   d.out = a->d_out;
-  HIP_TRY(launch_page_attend(d, a->d_ws, (hipStream_t)stream));
-  return DSI_OK;
+  return launched(launch_page_attend(d, a->d_ws, (hipStream_t)stream), "attention over pages");
 }
 
 dsi_status dsi_adjust(void* stream, const dsi_adjust_args* a) {
@@ -2401,8 +2402,6 @@ dsi_status dsi_adjust(void* stream, const dsi_adjust_args* a) {
   if (!a->n_windows || !a->rows) return DSI_OK;
   if ((long long)a->n_windows * a->rows * a->vocab > kMaxStepEntries)
     return fail(DSI_EINVAL, "n_windows*rows*vocab exceeds %lld", kMaxStepEntries);
-  if ((long long)a->n_windows * ((a->vocab - 1) / 4096 + 1) > kMaxStepChunks)
-    return fail(DSI_EINVAL, "n_windows * vocab / 4096 exceeds %d", kMaxStepChunks);
   const size_t esz = a->dtype == DSI_BF16 ? 2 : 4;
   DSI_TRY(rows_ok("logits", a->d_logits, a->ld, a->vocab, esz));
   DSI_TRY(rows_ok("output", a->d_out, a->ld_out, a->vocab, esz));
@@ -2435,8 +2434,7 @@ dsi_status dsi_adjust(void* stream, const dsi_adjust_args* a) {
   d.bias_ids = a->d_bias_ids;
   d.bias = a->d_bias;
   d.allowed = a->d_allowed;
-  HIP_TRY(launch_adjust(d, (hipStream_t)stream));
-  return DSI_OK;
+  return launched(launch_adjust(d, (hipStream_t)stream), "adjustment");
 }
 
 dsi_status dsi_kv_rollback(dsi_kv* kv, int32_t window, int32_t new_len) {

@@ -210,33 +210,38 @@ def test_attend_refuses_scales_that_are_infinite_to_the_base_2(stub):
 
 
 def test_sizes_that_no_launch_holds_are_refused(stub):
-    """A launch has fewer than 2^32 threads: the largest sizes taken, and those behind them."""
-    rope = dsi.make_rope(0, None)
-    far = dict(d_q=1 << 40, d_k=2 << 40, d_v=3 << 40, d_q_out=4 << 40)
-    pages = lambda **k: dsi.make_pages(**{**PAGES, "head_dim": 32, **k})  # noqa: E731
-    refused(dsi.dsi_page_append, dict(stream=0, rows=1 << 22, n_heads=0, rope=rope, **far), dict(pages=pages(n_kv_heads=33)), dict(pages=pages(n_kv_heads=1024)))
-    refused(dsi.dsi_page_attend_workspace, dict(pages=pages(n_kv_heads=256), rows=1 << 22, n_heads=256), dict(n_heads=512), dict(pages=pages(n_kv_heads=512), n_heads=512))
-    adjust = dict(stream=0, d_logits=1 << 40, d_out=1 << 40, dtype=dsi.DSI_BF16, rows=1)
-    refused(dsi.dsi_adjust, adjust, dict(n_windows=1 << 22, vocab=4 * 4096), dict(n_windows=1 << 20, vocab=128256))
+    """A launch has fewer than 2^24 workgroups of 256 (one of 2^24 + 5 runs five of them without an error): the largest sizes
+    that are taken, and those behind them, of which nothing is launched."""
     run(stub, '''
     def blocks(call):
         hip.stub_clear()
         call()
-        all_ = [g[0] for _, _, g in launches()]
-        assert max(all_) * 256 < 2 ** 32, all_
-        return max(all_)
-    rope = dsi.make_rope(0, None)
+        return max(g[0] for _, _, g in launches())
+    def none(call):
+        hip.stub_clear()
+        try:
+            call()
+        except dsi.DsiError as e:
+            assert e.status == dsi.DSI_EINVAL and not launches(), (e, launches())
+        else:
+            raise AssertionError("taken")
     far = [x << 40 for x in range(1, 6)]
-    for n_kv, windows in ((32, 1), (32, 4096)):
-        pages = dsi.make_pages(n_kv, 32, dsi.DSI_BF16, 100, 64, 1 << 20, 2 << 20, windows, 8, P, P, P)
-        assert blocks(lambda: dsi.dsi_page_append(0, pages, 1 << 22, 1, *far[:4], rope)) > 1 << 22
-    pages = dsi.make_pages(1024, 32, dsi.DSI_BF16, 100, 64, 1 << 20, 2 << 20, 4096, 8, P, P, P)
-    assert blocks(lambda: dsi.dsi_page_append(0, pages, 1 << 17, 1024, *far[:4], rope)) > 1 << 22
-    for n_kv, hq, rows in ((256, 256, 1 << 22), (1024, 1024, 1 << 20), (16, 1024, 1 << 20)):
-        for windows in (1, 4096):
-            pages = dsi.make_pages(n_kv, 32, dsi.DSI_BF16, 100, 64, 1 << 20, 2 << 20, windows, 8, P, P, P)
-            n = dsi.dsi_page_attend_workspace(pages, rows, hq)
-            assert blocks(lambda: dsi.dsi_page_attend(0, pages, rows, hq, far[0], far[1], far[2], n, dsi.DSI_BF16)) >= 1 << 23
-    assert blocks(lambda: dsi.dsi_adjust(0, 1 << 22, 1, 3 * 4096, far[0], far[0], dsi.DSI_BF16)) == 3 << 22
-    assert blocks(lambda: dsi.dsi_adjust(0, 1 << 17, 8, 127 * 4096, far[0], far[0], dsi.DSI_BF16)) == 127 << 17
+    pages = lambda n_kv, windows: dsi.make_pages(n_kv, 32, dsi.DSI_BF16, 100, 64, 1 << 20, 2 << 20, windows, 8, P, P, P)
+    append = lambda n_kv, windows, rows: lambda: dsi.dsi_page_append(0, pages(n_kv, windows), rows, 1, *far[:4], dsi.make_rope(0, None))
+    assert blocks(append(119, 1, 1 << 22)) == 119 * (2 + (1 << 22) // 32 - 1) + (1 << 20)
+    none(append(120, 1, 1 << 22))
+    none(append(1024, 4096, 1 << 19))
+    def attend(n_kv, hq, windows, rows):
+        p = pages(n_kv, windows)
+        n = dsi.dsi_page_attend_workspace(p, rows, hq)
+        return lambda: dsi.dsi_page_attend(0, p, rows, hq, far[0], far[1], far[2], n, dsi.DSI_BF16)
+    assert 511 << 15 < blocks(attend(511, 511, 1, 1 << 22)) < 1 << 24
+    assert 440 << 15 < blocks(attend(440, 440, 4096, 1 << 22)) < 1 << 24
+    none(attend(512, 512, 1, 1 << 22))
+    none(attend(456, 456, 4096, 1 << 22))
+    adjust = lambda B, R, V: lambda: dsi.dsi_adjust(0, B, R, V, far[0], far[0], dsi.DSI_BF16)
+    assert blocks(adjust(1 << 22, 1, 3 * 4096)) == 3 << 22
+    assert blocks(adjust(1 << 17, 8, 127 * 4096)) == 127 << 17
+    none(adjust(1 << 22, 1, 4 * 4096))
+    none(adjust(1 << 17, 8, 127 * 4096 + 1))
     ''')
