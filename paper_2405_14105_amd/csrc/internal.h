@@ -501,7 +501,7 @@ struct PageArgs {
 };
 // Rotation of queries and keys, and their way into the pages (rotate.hip)
 struct RotateArgs {
-  int rows, nq, nk, nv, hd, bf16;
+  int rows, nq, nk, hd, bf16;
   size_t ldq, ldk, ldv, ldqo, ldko;   // entries
   const void* q;
   const void* k;

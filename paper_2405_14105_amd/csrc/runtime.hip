@@ -2324,7 +2324,6 @@ dsi_status dsi_page_append(void* stream, const dsi_pages* pages, const dsi_page_
   if (a->n_heads && (!rows_apart(a->d_k, a->ld_k, nk, a->d_q_out, a->ld_q_out, nq, a->rows, esz) ||
                      !rows_apart(a->d_v, a->ld_v, nk, a->d_q_out, a->ld_q_out, nq, a->rows, esz)))
     return fail(DSI_EINVAL, "the output of queries overlaps the keys or values");
-  r.nv = r.nk;
   r.q = a->d_q;
   r.k = a->d_k;
   r.v = a->d_v;
