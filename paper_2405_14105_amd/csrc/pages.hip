@@ -672,7 +672,7 @@ struct ManyShared {
 // by lane from `to` on, past the registers; in order with the wave's loads, and
 // complete once vmcnt says so
 __device__ __forceinline__ void load_lds(const void* from, uint32_t off, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(from), "s"(to) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(from), "s"(to) : "memory");
 }
 template <bool KVB, int HD, bool QB>
 __device__ __forceinline__ void many_item(const PageAttnArgs& a, const PageClass& cl, int block, ManyShared<KVB, HD>& sh) {
